@@ -238,6 +238,105 @@ int hivis_tree_accept(hivis_ctx *ctx, int32_t *n_accepted, int32_t *tokens);
  *      target_tokens. */
 int hivis_tree_accept_sample(hivis_ctx *ctx, float temperature, const float *u, int32_t *n_accepted, int32_t *tokens);
 
+/* ---- operators on callers' tensors: a paged cache in 4 bits, and log probabilities ----
+ *
+ * They need no context.  All pointers are device memory of the current device (EINVAL for anything else), work is only
+ * enqueued on hip_stream (a hipStream_t, NULL = default), nothing is allocated, and the calls may be captured into a graph.
+ * After a failure hivis_last_error(NULL) has the message (per host thread) and nothing was enqueued.
+ * Workspaces belong to the caller: zero-filled once before their first use, left ready for the next call by every call,
+ * never used by two calls that may run at the same time (two streams, two graphs replayed side by side: two workspaces).
+ *
+ * The cache is a pool of blocks of block_tokens rows; a sequence's blocks are listed in its row of a block table, and a
+ * row's place is its slot = block * block_tokens + offset.  Memory of a block, per key head in order:
+ *   key codes [block_tokens][head_dim / 2] | value codes, the same | key scales [block_tokens][head_dim / 32] | value scales.
+ * A code is 4 bits (dim 2i in the low half of byte i): sign (8) and the magnitudes 0, .5, 1, 1.5, 2, 3, 4, 6; the scale byte
+ * b of 32 consecutive dims stands for 2^(b - 127).  A group whose largest magnitude is a gets the smallest power of two s
+ * with a <= 7 s, within 2^-100 .. 2^125, every value the code nearest to value / s (ties to the even code); a NaN or an
+ * infinity in a group makes all of it NaN (b = 255).  One layer's pool per call: models keep one pool per layer and share
+ * table and slots. */
+typedef struct {
+    int32_t n_kv_heads;
+    int32_t head_dim;        /* 64 or 128 */
+    int32_t block_tokens;    /* 16, 32, 64, 128 or 256 */
+    int32_t n_blocks;        /* n_blocks * block_tokens < 2^31 */
+} hivis_kv4_shape;
+
+/* Bytes of a pool (which must start at a multiple of 16), or a negative HIVIS_E*.  A pool needs no initial contents. */
+int64_t hivis_kv4_pool_bytes(const hivis_kv4_shape *shape);
+
+/* Block tables and slots of the next call's rows, from lengths that stay on the GPU.  Sequence s keeps its first keep[s]
+ * rows and gets add[s] new ones behind them (add = 0: rows given back; keep = add = 0: all of them).
+ *   keep, add [n_seqs] in.   held [n_seqs] in/out: blocks the sequence holds (0 at first).
+ *   table [n_seqs][max_blocks] in/out: its blocks in order, -1 where there is none.
+ *   free_list [1 + n_blocks] in/out: the number of free blocks, then the blocks; the last one is taken first.
+ *   row_start [n_seqs + 1] out: the new rows of sequence s are rows row_start[s] .. row_start[s+1] - 1.
+ *   slots [max_rows] out: slot of every new row, -1 behind the last one.   positions [max_rows] out (may be NULL): its
+ *   position in its sequence, -1 behind the last one.
+ *   status [n_seqs] out: 0 served; 1 too few free blocks; 2 impossible (a length below zero, more rows kept than the blocks
+ *   held have, more than max_blocks blocks); 3 more new rows than max_rows.  A sequence that is not served has no new rows
+ *   and keeps what it held.
+ * Blocks are given back first, the last sequence's last block first, and then taken in order of the sequences: the same
+ * lengths give the same tables, and blocks taken by a call and given back by the next leave the list as it was.  Sequence s
+ * is refused (1, 3) exactly if the sequences up to and with s need more than there is.
+ * Errors: EINVAL, EHIP. */
+int hivis_kv4_plan(void *hip_stream, int32_t n_seqs, int32_t max_blocks, int32_t block_tokens, int32_t n_blocks, const int32_t *keep, const int32_t *add, int32_t *held,
+                   int32_t *table, int32_t *free_list, int32_t *row_start, int32_t *slots, int32_t *positions, int32_t max_rows, int32_t *status);
+
+/* Rows into the cache.  k, v: HIVIS_F32 or HIVIS_BF16, head h of row r at r * row_stride + h * head_stride (in values, both
+ * multiples of 8; the same for k and v), starting at multiples of 16 bytes.  slots [n_rows]: a slot outside the pool (-1)
+ * leaves its row out.  Two rows with the same slot leave one of the two in each group of 32 dims.
+ * Errors: EINVAL, EHIP. */
+int hivis_kv4_append(void *hip_stream, const hivis_kv4_shape *shape, int32_t dtype, const void *k, const void *v, int64_t row_stride, int64_t head_stride, int32_t n_rows,
+                     const int32_t *slots, void *pool);
+
+/* The held values of rows (exact in either type); rows whose slot is outside the pool are left as they were. */
+int hivis_kv4_read(void *hip_stream, const hivis_kv4_shape *shape, int32_t dtype, const void *pool, int32_t n_rows, const int32_t *slots, void *k, void *v, int64_t row_stride,
+                   int64_t head_stride);
+
+/* Attention of the last rows of every sequence over its cached rows: out[i, h] = sum_j softmax_j(scale q[i, h] . k[j, h / G])
+ * v[j, h / G], G = n_q_heads / n_kv_heads.  Rows row_start[s] .. row_start[s+1] - 1 of q are the last ones of the kv_len[s]
+ * cached rows of sequence s (append first) and row i sees the keys up to its own position; with a mask, all keys before the
+ * sequence's rows of this call and, of those, key j where bit j of mask[row] is set.  A row that sees nothing gives zeros;
+ * what a row does not see does not reach it, NaN included.  A table entry outside the pool leaves its keys out. */
+typedef struct {
+    hivis_kv4_shape cache;
+    int32_t dtype;           /* of q and out: HIVIS_F32 or HIVIS_BF16 */
+    int32_t n_q_heads;
+    int32_t n_seqs;
+    int32_t n_rows;          /* rows of q and out: a sequence whose row_start reaches beyond them is left out */
+    int32_t max_blocks;      /* entries of a sequence's row of the table */
+    int32_t max_rows;        /* most rows of one sequence in this call (at most 64 with a mask); rows beyond are not computed */
+    int32_t max_len;         /* most cached rows of one sequence: sizes the launch; longer ones are right, but slower */
+    float scale;
+    const void *pool;
+    const int32_t *table;    /* [n_seqs][max_blocks] */
+    const int32_t *row_start;/* [n_seqs + 1] */
+    const int32_t *kv_len;   /* [n_seqs] */
+    const void *q;           /* [rows][n_q_heads][head_dim], rows q_stride values apart */
+    int64_t q_stride;
+    const uint64_t *mask;    /* [rows], or NULL */
+    void *out;               /* as q, rows out_stride values apart; rows outside row_start's ranges are left as they were */
+    int64_t out_stride;
+    void *workspace;
+    int64_t workspace_bytes;
+} hivis_kv4_attention;
+
+/* Bytes of workspace for calls with these cache, n_q_heads, n_seqs, max_rows and max_len (the other fields are not read). */
+int64_t hivis_kv4_attend_bytes(const hivis_kv4_attention *a);
+
+/* Errors: EINVAL (also: starts no multiples of 16 bytes, strides no multiples of 8 values, of 4 for HIVIS_F32), EHIP. */
+int hivis_kv4_attend(void *hip_stream, const hivis_kv4_attention *a);
+
+/* Log probabilities of given tokens under softmax(logits / temperature), the entropy of each row (in nats), and its top_k
+ * most probable tokens (the larger logit first, then the lower id).
+ *   logits: HIVIS_F32 or HIVIS_BF16, [n_rows][vocab], rows row_stride values apart.   tokens [n_rows][n_tokens].
+ *   logprob [n_rows][n_tokens]; entropy [n_rows] (may be NULL); top_ids, top_logprobs [n_rows][top_k], top_k <= 32.
+ * A token outside [0, vocab) gives NaN.  A row with a NaN or without a finite maximum gives NaN everywhere and ids -1.
+ * Errors: EINVAL, EHIP. */
+int hivis_logprobs(void *hip_stream, int32_t dtype, const void *logits, int64_t row_stride, int32_t n_rows, int32_t vocab, float temperature, const int32_t *tokens, int32_t n_tokens,
+                   float *logprob, float *entropy, int32_t top_k, int32_t *top_ids, float *top_logprobs, void *workspace, int64_t workspace_bytes);
+int64_t hivis_logprobs_bytes(int32_t n_rows, int32_t vocab, int32_t top_k);
+
 /* ---- test / measurement hooks (all synchronise) ---- */
 
 /* The last tree, any pointer may be null (host arrays): pool_tokens / pool_parents (pool index, -1 = root) /

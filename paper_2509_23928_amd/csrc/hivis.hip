@@ -9,6 +9,7 @@
 #include "hivis_tile.h"
 #include "hivis_attn.h"
 #include "hivis_tree.h"
+#include "hivis_ops.h"
 
 #include <hip/hip_ext.h>
 #include <algorithm>
@@ -2344,6 +2345,8 @@ int check_config(const hivis_config* g, std::string& why) {
 thread_local std::string g_create_err;
 
 }  // namespace
+
+namespace hivis { void set_thread_error(const char* message) { g_create_err = message; } }
 
 #define DISPATCH(c, fn, ...) ((c)->cfg.dtype == HIVIS_BF16 ? fn<bf16_t>(__VA_ARGS__) : fn<float>(__VA_ARGS__))
 

@@ -1,0 +1,22 @@
+// What the contexts (hivis.hip) use of the operators (hivis_ops.hip): launches without the checks of callers' arguments.
+#pragma once
+#include <hip/hip_runtime.h>
+
+namespace hivis {
+
+struct PlanArgs; struct RowsArgs; struct Kv4AttnArgs; struct LogprobsArgs; struct Kv4Dims;
+
+enum { KV4_ROWS_F32 = 0, KV4_ROWS_BF16 = 1, KV4_ROWS_HALVES = 2 };
+
+void set_thread_error(const char* message);                  // what hivis_last_error(NULL) returns on this thread
+int op_fail(int code, const char* fmt, ...);
+
+int kv4_plan_launch(hipStream_t st, const PlanArgs& a);
+int kv4_append_launch(hipStream_t st, int type, const RowsArgs& a);
+int kv4_read_launch(hipStream_t st, int type, const RowsArgs& a);
+int kv4_attend_launch(hipStream_t st, int dtype, Kv4AttnArgs a, int max_rows, int max_len, void* ws, long long ws_bytes);
+long long kv4_attend_space(const Kv4Dims& d, int n_q_heads, int n_seqs, int max_rows, int max_len);
+int logprobs_launch(hipStream_t st, int dtype, const LogprobsArgs& a, void* ws, long long ws_bytes);
+long long logprobs_space(int rows, int vocab, int top);
+
+}  // namespace hivis

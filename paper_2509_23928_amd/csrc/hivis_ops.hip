@@ -1,0 +1,251 @@
+// Host side of the operators that work on callers' tensors: the paged cache in 4 bits and the log probabilities.  The C ABI is declared and documented in include/hivis.h.
+#include "hivis.h"
+#include "hivis_kv4.h"
+#include "hivis_logprobs.h"
+#include "hivis_ops.h"
+
+#include <algorithm>
+#include <cmath>
+#include <cstdarg>
+#include <cstdio>
+#include <string>
+
+using namespace hivis;
+
+namespace hivis {
+
+int op_fail(int code, const char* fmt, ...) {
+    char buf[512];
+    va_list ap; va_start(ap, fmt); vsnprintf(buf, sizeof buf, fmt, ap); va_end(ap);
+    set_thread_error(buf);
+    return code;
+}
+
+}  // namespace hivis
+
+namespace {
+
+#define OP_TRY(expr)                                                                                              \
+    do {                                                                                                          \
+        hipError_t e_ = (expr);                                                                                   \
+        if (e_ != hipSuccess) return op_fail(HIVIS_EHIP, "%s failed: %s", #expr, hipGetErrorString(e_));          \
+    } while (0)
+#define CHECK(cond, ...) do { if (!(cond)) return op_fail(HIVIS_EINVAL, __VA_ARGS__); } while (0)
+
+// Memory of the current device: the kernels run there, and a host address or another device's would fault.
+int check_device(const void* p, const char* what, int dev) {
+    hipPointerAttribute_t at{};
+    const hipError_t e = hipPointerGetAttributes(&at, p);
+    if (e != hipSuccess) { (void)hipGetLastError(); return op_fail(HIVIS_EINVAL, "%s is not device memory", what); }
+    if (at.type != hipMemoryTypeDevice && at.type != hipMemoryTypeManaged) return op_fail(HIVIS_EINVAL, "%s is not device memory", what);
+    if (at.device != dev) return op_fail(HIVIS_EINVAL, "%s is on device %d, the current device is %d", what, at.device, dev);
+    return HIVIS_OK;
+}
+struct Named { const void* p; const char* name; };
+int check_devices(std::initializer_list<Named> list) {
+    int dev = 0;
+    OP_TRY(hipGetDevice(&dev));
+    for (const Named& n : list)
+        if (n.p) if (int rc = check_device(n.p, n.name, dev)) return rc;
+    return HIVIS_OK;
+}
+bool aligned(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
+
+int check_shape(const hivis_kv4_shape* s, Kv4Dims* d) {
+    CHECK(s, "null shape");
+    CHECK(s->head_dim == 64 || s->head_dim == 128, "head_dim %d not in {64,128}", s->head_dim);
+    CHECK(s->n_kv_heads >= 1 && s->n_kv_heads <= 65535, "n_kv_heads %d outside [1,65535]", s->n_kv_heads);
+    CHECK(s->block_tokens >= 16 && s->block_tokens <= 256 && !(s->block_tokens & (s->block_tokens - 1)), "block_tokens %d not in {16,32,64,128,256}", s->block_tokens);
+    CHECK(s->n_blocks >= 1 && (long long)s->n_blocks * s->block_tokens <= 0x7fffffffLL, "n_blocks %d: the slots of a pool must be in 1..2^31-1", s->n_blocks);
+    *d = Kv4Dims{s->n_kv_heads, s->head_dim, s->block_tokens, __builtin_ctz(s->block_tokens), s->n_blocks};
+    return HIVIS_OK;
+}
+
+int check_rows(const void* k, const void* v, int dtype, const Kv4Dims& d, long long row, long long head, int n) {
+    CHECK(dtype == HIVIS_F32 || dtype == HIVIS_BF16, "dtype %d unknown", dtype);
+    CHECK(n >= 0 && (long long)n * d.heads <= 0x7fffffffLL, "n_rows %d x n_kv_heads %d", n, d.heads);
+    CHECK(row % 8 == 0 && head % 8 == 0, "row and head strides must be multiples of 8 values (%lld, %lld)", row, head);
+    CHECK(row >= 0 && head >= d.hd, "strides %lld, %lld: rows of a head are head_dim values side by side", row, head);
+    CHECK(aligned(k, 16) && aligned(v, 16), "rows must start at multiples of 16 bytes");
+    return HIVIS_OK;
+}
+
+
+}  // namespace
+
+namespace hivis {
+
+int kv4_plan_launch(hipStream_t st, const PlanArgs& a) {
+    hipLaunchKernelGGL(kv4_plan_kernel, dim3(1), dim3(PLAN_NT), 0, st, a);
+    OP_TRY(hipGetLastError());
+    return HIVIS_OK;
+}
+
+static dim3 rows_grid(const RowsArgs& a) { return dim3((unsigned)(((long long)a.n * a.d.heads * 2 * (a.d.hd / 8) + 255) / 256)); }
+
+int kv4_append_launch(hipStream_t st, int type, const RowsArgs& a) {
+    if (a.n == 0) return HIVIS_OK;
+    if (type == KV4_ROWS_F32) hipLaunchKernelGGL(kv4_append_kernel<float>, rows_grid(a), dim3(256), 0, st, a);
+    else if (type == KV4_ROWS_BF16) hipLaunchKernelGGL(kv4_append_kernel<__bf16>, rows_grid(a), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL(kv4_append_kernel<Kv4Halves>, rows_grid(a), dim3(256), 0, st, a);
+    OP_TRY(hipGetLastError());
+    return HIVIS_OK;
+}
+
+int kv4_read_launch(hipStream_t st, int type, const RowsArgs& a) {
+    if (a.n == 0) return HIVIS_OK;
+    if (type == KV4_ROWS_F32) hipLaunchKernelGGL(kv4_read_kernel<float>, rows_grid(a), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL(kv4_read_kernel<__bf16>, rows_grid(a), dim3(256), 0, st, a);
+    OP_TRY(hipGetLastError());
+    return HIVIS_OK;
+}
+
+int kv4_attend_launch(hipStream_t st, int dtype, Kv4AttnArgs a, int max_rows, int max_len, void* ws, long long ws_bytes) {
+    (void)max_len; (void)ws; (void)ws_bytes;
+    a.tiles = (int)(((long long)max_rows * a.group + 15) / 16);
+    const long long wgs = (long long)a.n_seqs * a.tiles * a.d.heads;
+    if (wgs == 0) return HIVIS_OK;
+    if (wgs > 0x7fffffffLL) return op_fail(HIVIS_EINVAL, "%lld work items are more than a launch takes", wgs);
+#define KV4_ATTEND(T_, HD_) hipLaunchKernelGGL((kv4_attend_kernel<T_, HD_>), dim3((unsigned)wgs), dim3(256), 0, st, a)
+    if (dtype == HIVIS_F32) { if (a.d.hd == 128) KV4_ATTEND(float, 128); else KV4_ATTEND(float, 64); }
+    else { if (a.d.hd == 128) KV4_ATTEND(__bf16, 128); else KV4_ATTEND(__bf16, 64); }
+#undef KV4_ATTEND
+    OP_TRY(hipGetLastError());
+    return HIVIS_OK;
+}
+
+long long kv4_attend_space(const Kv4Dims& d, int n_q_heads, int n_seqs, int max_rows, int max_len) {
+    (void)d; (void)n_q_heads; (void)n_seqs; (void)max_rows; (void)max_len;
+    return 16;
+}
+
+int logprobs_launch(hipStream_t st, int dtype, const LogprobsArgs& a, void* ws, long long ws_bytes) {
+    (void)ws; (void)ws_bytes;
+    if (a.rows == 0) return HIVIS_OK;
+    if (dtype == HIVIS_F32) hipLaunchKernelGGL(logprobs_kernel<float>, dim3(a.rows), dim3(1024), 0, st, a);
+    else hipLaunchKernelGGL(logprobs_kernel<__bf16>, dim3(a.rows), dim3(1024), 0, st, a);
+    OP_TRY(hipGetLastError());
+    return HIVIS_OK;
+}
+
+long long logprobs_space(int rows, int vocab, int top) { (void)rows; (void)vocab; (void)top; return 16; }
+
+}  // namespace hivis
+
+extern "C" {
+
+int64_t hivis_kv4_pool_bytes(const hivis_kv4_shape* shape) {
+    Kv4Dims d;
+    if (int rc = check_shape(shape, &d)) return rc;
+    return (int64_t)d.n_blocks * d.heads * kv4_chunk(d.hd, d.block);
+}
+
+int hivis_kv4_plan(void* hip_stream, int32_t n_seqs, int32_t max_blocks, int32_t block_tokens, int32_t n_blocks, const int32_t* keep, const int32_t* add, int32_t* held,
+                   int32_t* table, int32_t* free_list, int32_t* row_start, int32_t* slots, int32_t* positions, int32_t max_rows, int32_t* status) {
+    hivis_kv4_shape shape{1, 64, block_tokens, n_blocks};
+    Kv4Dims d;
+    if (int rc = check_shape(&shape, &d)) return rc;
+    CHECK(n_seqs >= 1, "n_seqs %d", n_seqs);
+    CHECK(max_blocks >= 1 && (long long)max_blocks * block_tokens <= 0x7fffffffLL, "max_blocks %d: a sequence's positions must be in 0..2^31-1", max_blocks);
+    CHECK(max_rows >= 0, "max_rows %d", max_rows);
+    CHECK(keep && add && held && table && free_list && row_start && status && (slots || max_rows == 0), "null argument");
+    if (int rc = check_devices({{keep, "keep"}, {add, "add"}, {held, "held"}, {table, "table"}, {free_list, "free_list"}, {row_start, "row_start"}, {slots, "slots"},
+                                {positions, "positions"}, {status, "status"}})) return rc;
+    return kv4_plan_launch((hipStream_t)hip_stream, PlanArgs{n_seqs, max_blocks, d.shift, n_blocks, max_rows, keep, add, held, table, free_list, row_start, slots, positions, status});
+}
+
+int hivis_kv4_append(void* hip_stream, const hivis_kv4_shape* shape, int32_t dtype, const void* k, const void* v, int64_t row_stride, int64_t head_stride, int32_t n_rows,
+                     const int32_t* slots, void* pool) {
+    RowsArgs a{};
+    if (int rc = check_shape(shape, &a.d)) return rc;
+    CHECK(n_rows == 0 || (k && v && slots && pool), "null argument");
+    if (int rc = check_rows(k, v, dtype, a.d, row_stride, head_stride, n_rows)) return rc;
+    CHECK(aligned(pool, 16), "the pool must start at a multiple of 16 bytes");
+    if (int rc = check_devices({{k, "k"}, {v, "v"}, {slots, "slots"}, {pool, "pool"}})) return rc;
+    a.k = k; a.v = v; a.row = row_stride; a.head = head_stride; a.n = n_rows; a.slots = slots; a.pool = (uint8_t*)pool;
+    return kv4_append_launch((hipStream_t)hip_stream, dtype == HIVIS_F32 ? KV4_ROWS_F32 : KV4_ROWS_BF16, a);
+}
+
+int hivis_kv4_read(void* hip_stream, const hivis_kv4_shape* shape, int32_t dtype, const void* pool, int32_t n_rows, const int32_t* slots, void* k, void* v, int64_t row_stride,
+                   int64_t head_stride) {
+    RowsArgs a{};
+    if (int rc = check_shape(shape, &a.d)) return rc;
+    CHECK(n_rows == 0 || (k && v && slots && pool), "null argument");
+    if (int rc = check_rows(k, v, dtype, a.d, row_stride, head_stride, n_rows)) return rc;
+    CHECK(aligned(pool, 16), "the pool must start at a multiple of 16 bytes");
+    if (int rc = check_devices({{k, "k"}, {v, "v"}, {slots, "slots"}, {pool, "pool"}})) return rc;
+    a.k = k; a.v = v; a.row = row_stride; a.head = head_stride; a.n = n_rows; a.slots = slots; a.pool = (uint8_t*)const_cast<void*>(pool);
+    return kv4_read_launch((hipStream_t)hip_stream, dtype == HIVIS_F32 ? KV4_ROWS_F32 : KV4_ROWS_BF16, a);
+}
+
+static int check_attention(const hivis_kv4_attention* a, Kv4Dims* d) {
+    CHECK(a, "null argument");
+    if (int rc = check_shape(&a->cache, d)) return rc;
+    CHECK(a->dtype == HIVIS_F32 || a->dtype == HIVIS_BF16, "dtype %d unknown", a->dtype);
+    CHECK(a->n_q_heads >= 1 && a->n_q_heads % d->heads == 0, "n_q_heads %d is no multiple of n_kv_heads %d", a->n_q_heads, d->heads);
+    CHECK(a->n_seqs >= 0 && a->max_rows >= 0 && a->max_len >= 0, "n_seqs %d, max_rows %d, max_len %d", a->n_seqs, a->max_rows, a->max_len);
+    CHECK((long long)a->max_rows * a->n_q_heads <= 0x7fffffffLL / 128, "max_rows %d x n_q_heads %d", a->max_rows, a->n_q_heads);
+    return HIVIS_OK;
+}
+
+int64_t hivis_kv4_attend_bytes(const hivis_kv4_attention* a) {
+    Kv4Dims d;
+    if (int rc = check_attention(a, &d)) return rc;
+    return kv4_attend_space(d, a->n_q_heads, a->n_seqs, a->max_rows, a->max_len);
+}
+
+int hivis_kv4_attend(void* hip_stream, const hivis_kv4_attention* a) {
+    Kv4AttnArgs k{};
+    if (int rc = check_attention(a, &k.d)) return rc;
+    CHECK(a->n_rows >= 0 && (long long)a->n_rows * a->n_q_heads <= 0x7fffffffLL, "n_rows %d x n_q_heads %d", a->n_rows, a->n_q_heads);
+    if (a->n_seqs == 0 || a->max_rows == 0 || a->n_rows == 0) return HIVIS_OK;
+    CHECK(a->max_blocks >= 1 && (long long)a->max_blocks * k.d.block <= 0x7fffffffLL, "max_blocks %d: a sequence's positions must be in 0..2^31-1", a->max_blocks);
+    CHECK(!a->mask || a->max_rows <= 64, "max_rows %d: a mask has bits for 64 rows", a->max_rows);
+    CHECK(std::isfinite(a->scale), "scale is not finite");
+    const int align = a->dtype == HIVIS_F32 ? 4 : 8;
+    const long long width = (long long)a->n_q_heads * k.d.hd;
+    CHECK(a->q_stride % align == 0 && a->q_stride >= 0 && a->out_stride >= width && a->out_stride % align == 0,
+          "row strides %lld, %lld: multiples of %d values, of the output not below n_q_heads * head_dim", (long long)a->q_stride, (long long)a->out_stride, align);
+    CHECK(a->pool && a->table && a->row_start && a->kv_len && a->q && a->out && a->workspace, "null argument");
+    CHECK(aligned(a->pool, 16) && aligned(a->q, 16) && aligned(a->out, 16) && aligned(a->workspace, 16), "pool, q, out and workspace must start at multiples of 16 bytes");
+    const long long need = kv4_attend_space(k.d, a->n_q_heads, a->n_seqs, a->max_rows, a->max_len);
+    CHECK(a->workspace_bytes >= need, "workspace of %lld bytes, %lld needed", (long long)a->workspace_bytes, need);
+    if (int rc = check_devices({{a->pool, "pool"}, {a->table, "table"}, {a->row_start, "row_start"}, {a->kv_len, "kv_len"}, {a->q, "q"}, {a->mask, "mask"}, {a->out, "out"},
+                                {a->workspace, "workspace"}})) return rc;
+    k.group = a->n_q_heads / k.d.heads; k.n_seqs = a->n_seqs; k.n_rows = a->n_rows; k.max_blocks = a->max_blocks; k.scale2 = (float)(a->scale * 1.4426950408889634);
+    k.pool = (const uint8_t*)a->pool; k.table = a->table; k.row_start = a->row_start; k.kv_len = a->kv_len; k.q = a->q; k.ldq = a->q_stride;
+    k.mask = (const unsigned long long*)a->mask; k.out = a->out; k.ldo = a->out_stride;
+    return kv4_attend_launch((hipStream_t)hip_stream, a->dtype, k, a->max_rows, a->max_len, a->workspace, a->workspace_bytes);
+}
+
+static int check_logprobs(int32_t n_rows, int32_t vocab, int32_t top_k) {
+    CHECK(n_rows >= 0 && vocab >= 1, "n_rows %d, vocab %d", n_rows, vocab);
+    CHECK(top_k >= 0 && top_k <= LOGPROBS_MAX_TOP && top_k <= vocab, "top_k %d outside [0,%d] or above vocab %d", top_k, LOGPROBS_MAX_TOP, vocab);
+    return HIVIS_OK;
+}
+
+int64_t hivis_logprobs_bytes(int32_t n_rows, int32_t vocab, int32_t top_k) {
+    if (int rc = check_logprobs(n_rows, vocab, top_k)) return rc;
+    return logprobs_space(n_rows, vocab, top_k);
+}
+
+int hivis_logprobs(void* hip_stream, int32_t dtype, const void* logits, int64_t row_stride, int32_t n_rows, int32_t vocab, float temperature, const int32_t* tokens, int32_t n_tokens,
+                   float* logprob, float* entropy, int32_t top_k, int32_t* top_ids, float* top_logprobs, void* workspace, int64_t workspace_bytes) {
+    if (int rc = check_logprobs(n_rows, vocab, top_k)) return rc;
+    CHECK(dtype == HIVIS_F32 || dtype == HIVIS_BF16, "dtype %d unknown", dtype);
+    CHECK(row_stride >= vocab, "row_stride %lld below vocab %d", (long long)row_stride, vocab);
+    const float inv = 1.f / temperature;
+    CHECK(temperature > 0.f && inv > 0.f && std::isfinite(inv), "temperature %g: it and its reciprocal must be positive and finite", (double)temperature);
+    CHECK(n_tokens >= 0 && (n_tokens == 0 || (tokens && logprob)) && (top_k == 0 || (top_ids && top_logprobs)), "null argument");
+    if (n_rows == 0) return HIVIS_OK;
+    CHECK(logits && workspace, "null argument");
+    CHECK(aligned(logits, dtype == HIVIS_F32 ? 4 : 2) && aligned(workspace, 16), "logits must start at a multiple of their size, the workspace at one of 16 bytes");
+    const long long need = logprobs_space(n_rows, vocab, top_k);
+    CHECK(workspace_bytes >= need, "workspace of %lld bytes, %lld needed", (long long)workspace_bytes, need);
+    if (int rc = check_devices({{logits, "logits"}, {n_tokens ? tokens : nullptr, "tokens"}, {n_tokens ? logprob : nullptr, "logprob"}, {entropy, "entropy"}, {top_k ? top_ids : nullptr, "top_ids"},
+                                {top_k ? top_logprobs : nullptr, "top_logprobs"}, {workspace, "workspace"}})) return rc;
+    return logprobs_launch((hipStream_t)hip_stream, dtype,
+                           LogprobsArgs{logits, row_stride, n_rows, vocab, inv, tokens, n_tokens, logprob, entropy, top_k, top_ids, top_logprobs}, workspace, workspace_bytes);
+}
+
+}  // extern "C"
