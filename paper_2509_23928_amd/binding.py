@@ -164,101 +164,109 @@ def _op(rc):
     return rc
 
 
-def _dtype(name):
+_kinds = {}                                  # type objects by their names ("float32", ...): a name is made once, not per call
+
+
+def _kind(dtype):
+    kind = _kinds.get(dtype)
+    if kind is None:
+        kind = _kinds[dtype] = str(dtype).split(".")[-1]
+    return kind
+
+
+def _dtype(dtype):
     """HIVIS_F32 or HIVIS_BF16 of a tensor type."""
-    kind = str(name).split(".")[-1]
-    if kind not in ("float32", "bfloat16"):
-        _refuse(f"type {name} is neither float32 nor bfloat16")
+    kind = _kind(dtype)
+    if kind != "float32" and kind != "bfloat16":
+        _refuse(f"type {dtype} is neither float32 nor bfloat16")
     return HIVIS_F32 if kind == "float32" else HIVIS_BF16
 
 
 def _tensor(t, kind, shape, name):
-    """Address of a contiguous tensor of this type and shape (None in shape: any; t None: no tensor)."""
+    """Address of a contiguous tensor of this type and shape (shape None: any one-dimensional; t None: no tensor)."""
     if t is None:
         return None
-    if str(t.dtype).split(".")[-1] != kind:
+    if _kind(t.dtype) != kind:
         _refuse(f"{name}: {t.dtype} instead of {kind}")
-    if len(t.shape) != len(shape) or any(w is not None and int(w) != int(g) for w, g in zip(shape, t.shape)):
+    if t.shape != shape and (shape is not None or len(t.shape) != 1):
         _refuse(f"{name}: shape {tuple(t.shape)} instead of {shape}")
     if not t.is_contiguous():
         _refuse(f"{name} is not contiguous")
-    return _ptr(t)
+    return t.data_ptr()
 
 
 def kv4_pool_bytes(shape):
     """Bytes of one layer's pool of this Kv4Shape."""
-    return int(_op(load_library().hivis_kv4_pool_bytes(C.byref(shape))))
+    return _op(load_library().hivis_kv4_pool_bytes(C.byref(shape)))
 
 
 def kv4_plan(keep, add, held, table, free_list, row_start, slots, positions, status, *, block_tokens, n_blocks, stream=None):
     """hivis_kv4_plan: block tables, slots and positions (None: not wanted) of the next call's rows.  int32 tensors."""
     if len(table.shape) != 2 or len(slots.shape) != 1:
         _refuse("table is [n_seqs][max_blocks], slots [max_rows]")
-    n, blocks, rows = int(table.shape[0]), int(table.shape[1]), int(slots.shape[0])
-    t = lambda x, shape, name: _tensor(x, "int32", shape, name)
-    _op(load_library().hivis_kv4_plan(C.c_void_p(stream or 0), n, blocks, int(block_tokens), int(n_blocks), t(keep, (n,), "keep"), t(add, (n,), "add"), t(held, (n,), "held"),
-                                      t(table, (n, blocks), "table"), t(free_list, (int(n_blocks) + 1,), "free_list"), t(row_start, (n + 1,), "row_start"),
-                                      t(slots, (rows,), "slots"), t(positions, (rows,), "positions"), rows, t(status, (n,), "status")))
+    n, blocks = table.shape
+    rows = slots.shape[0]
+    t = _tensor
+    _op(load_library().hivis_kv4_plan(stream, n, blocks, block_tokens, n_blocks, t(keep, "int32", (n,), "keep"), t(add, "int32", (n,), "add"), t(held, "int32", (n,), "held"),
+                                      t(table, "int32", (n, blocks), "table"), t(free_list, "int32", (n_blocks + 1,), "free_list"), t(row_start, "int32", (n + 1,), "row_start"),
+                                      t(slots, "int32", (rows,), "slots"), t(positions, "int32", (rows,), "positions"), rows, t(status, "int32", (n,), "status")))
 
 
 def _kv4_rows(shape, pool, slots, k, v):
-    rows = int(slots.shape[0])
-    want = (rows, shape.n_kv_heads, shape.head_dim)
-    for x, name in ((k, "k"), (v, "v")):
-        if tuple(x.shape) != want:
-            _refuse(f"{name}: shape {tuple(x.shape)} instead of {want}")
-        if rows and x.stride(2) != 1:
-            _refuse(f"{name}: the values of a head are not side by side")
-    if k.dtype != v.dtype or (rows and k.stride()[:2] != v.stride()[:2]):
+    rows, heads, hd = slots.shape[0], shape.n_kv_heads, shape.head_dim
+    want = (rows, heads, hd)
+    if k.shape != want or v.shape != want:
+        _refuse(f"k {tuple(k.shape)}, v {tuple(v.shape)} instead of {want}")
+    row, head, one = k.stride()
+    if k.dtype != v.dtype or (rows and (row, head, one) != v.stride()):
         _refuse("k and v differ in type or strides")
-    row, head = (k.stride(0), k.stride(1)) if rows else (0, shape.head_dim)
+    if rows and one != 1:
+        _refuse("k, v: the values of a head are not side by side")
     # a dimension of one element has any stride
-    head = head if shape.n_kv_heads > 1 else shape.head_dim
-    row = row if rows > 1 else 0
-    return _dtype(k.dtype), _tensor(pool, "uint8", (kv4_pool_bytes(shape),), "pool"), _tensor(slots, "int32", (rows,), "slots"), rows, row, head
+    return (_dtype(k.dtype), _tensor(pool, "uint8", (kv4_pool_bytes(shape),), "pool"), _tensor(slots, "int32", (rows,), "slots"), rows, row if rows > 1 else 0,
+            head if heads > 1 and rows else hd)
 
 
 def kv4_append(shape, pool, slots, k, v, *, stream=None):
     """hivis_kv4_append: rows k, v [rows][n_kv_heads][head_dim] (float32 or bfloat16, any strides of rows and heads that are multiples of 8) into
     the pool (uint8) at slots [rows] int32."""
     dtype, p, s, rows, row, head = _kv4_rows(shape, pool, slots, k, v)
-    _op(load_library().hivis_kv4_append(C.c_void_p(stream or 0), C.byref(shape), dtype, _ptr(k), _ptr(v), row, head, rows, s, p))
+    _op(load_library().hivis_kv4_append(stream, C.byref(shape), dtype, k.data_ptr(), v.data_ptr(), row, head, rows, s, p))
 
 
 def kv4_read(shape, pool, slots, k, v, *, stream=None):
     """hivis_kv4_read: the held values of the rows at slots into k and v."""
     dtype, p, s, rows, row, head = _kv4_rows(shape, pool, slots, k, v)
-    _op(load_library().hivis_kv4_read(C.c_void_p(stream or 0), C.byref(shape), dtype, p, rows, s, _ptr(k), _ptr(v), row, head))
+    _op(load_library().hivis_kv4_read(stream, C.byref(shape), dtype, p, rows, s, k.data_ptr(), v.data_ptr(), row, head))
 
 
 def kv4_attend_bytes(shape, n_q_heads, n_seqs, max_rows, max_len, dtype):
-    """Bytes of the (zero-filled) workspace of kv4_attend calls up to these sizes; dtype: of q."""
+    """Bytes of the (zero-filled) workspace of kv4_attend calls of these sizes; dtype: of q."""
     a = hivis_kv4_attention(cache=shape, dtype=_dtype(dtype), n_q_heads=int(n_q_heads), n_seqs=int(n_seqs), max_rows=int(max_rows), max_len=int(max_len))
-    return int(_op(load_library().hivis_kv4_attend_bytes(C.byref(a))))
+    return _op(load_library().hivis_kv4_attend_bytes(C.byref(a)))
 
 
 def kv4_attend(shape, pool, table, row_start, kv_len, q, out, *, max_rows, max_len, workspace, scale=None, mask=None, stream=None):
     """hivis_kv4_attend: attention of q [rows][n_q_heads][head_dim] over the cached rows, to out (as q).  table [n_seqs][max_blocks], row_start
     [n_seqs + 1], kv_len [n_seqs] int32; mask [rows] int64 or None; scale None: 1 / sqrt(head_dim)."""
-    if len(q.shape) != 3 or q.shape[2] != shape.head_dim or tuple(out.shape) != tuple(q.shape) or out.dtype != q.dtype or len(table.shape) != 2:
+    if len(q.shape) != 3 or q.shape[2] != shape.head_dim or out.shape != q.shape or out.dtype != q.dtype or len(table.shape) != 2:
         _refuse(f"q {tuple(q.shape)} and out {tuple(out.shape)}: [rows][n_q_heads][{shape.head_dim}] of one type; table [n_seqs][max_blocks]")
-    rows, hq, hd = (int(x) for x in q.shape)
-    n, blocks = int(table.shape[0]), int(table.shape[1])
-    for x, name in ((q, "q"), (out, "out")):
-        if rows and (x.stride(2) != 1 or (hq > 1 and x.stride(1) != hd)):
-            _refuse(f"{name}: the heads of a row are not side by side")
-    i32 = lambda x, s, name: _tensor(x, "int32", s, name)
-    a = hivis_kv4_attention(cache=shape, dtype=_dtype(q.dtype), n_q_heads=hq, n_seqs=n, n_rows=rows, max_blocks=blocks, max_rows=int(max_rows), max_len=int(max_len),
-                            scale=float(hd ** -0.5 if scale is None else scale), pool=_tensor(pool, "uint8", (kv4_pool_bytes(shape),), "pool"),
-                            table=i32(table, (n, blocks), "table"), row_start=i32(row_start, (n + 1,), "row_start"), kv_len=i32(kv_len, (n,), "kv_len"),
-                            q=_ptr(q), q_stride=q.stride(0) if rows > 1 else hq * hd, mask=_tensor(mask, "int64", (rows,), "mask"), out=_ptr(out),
-                            out_stride=out.stride(0) if rows > 1 else hq * hd, workspace=_tensor(workspace, "uint8", (None,), "workspace"), workspace_bytes=int(workspace.shape[0]))
-    _op(load_library().hivis_kv4_attend(C.c_void_p(stream or 0), C.byref(a)))
+    rows, hq, hd = q.shape
+    n, blocks = table.shape
+    ldq, ldo = q.stride(), out.stride()
+    if rows and (ldq[2] != 1 or ldo[2] != 1 or (hq > 1 and (ldq[1] != hd or ldo[1] != hd))):
+        _refuse("q, out: the heads of a row are not side by side")
+    t = _tensor
+    a = hivis_kv4_attention(shape, _dtype(q.dtype), hq, n, rows, blocks, max_rows, max_len, hd ** -0.5 if scale is None else scale, t(pool, "uint8", (kv4_pool_bytes(shape),), "pool"),
+                            t(table, "int32", (n, blocks), "table"), t(row_start, "int32", (n + 1,), "row_start"), t(kv_len, "int32", (n,), "kv_len"), q.data_ptr(),
+                            ldq[0] if rows > 1 else hq * hd, t(mask, "int64", (rows,), "mask"), out.data_ptr(), ldo[0] if rows > 1 else hq * hd,
+                            t(workspace, "uint8", None, "workspace"), workspace.shape[0])
+    _op(load_library().hivis_kv4_attend(stream, C.byref(a)))
 
 
 def logprobs_bytes(n_rows, vocab, top_k=0):
     """Bytes of the (zero-filled) workspace of logprobs calls of these sizes."""
-    return int(_op(load_library().hivis_logprobs_bytes(int(n_rows), int(vocab), int(top_k))))
+    return _op(load_library().hivis_logprobs_bytes(int(n_rows), int(vocab), int(top_k)))
 
 
 def logprobs(logits, tokens, logprob, entropy=None, top_ids=None, top_logprobs=None, *, workspace, temperature=1.0, stream=None):
@@ -266,18 +274,18 @@ def logprobs(logits, tokens, logprob, entropy=None, top_ids=None, top_logprobs=N
     top_logprobs [rows][k] where given.  logits [rows][vocab] float32 or bfloat16, any row stride."""
     if len(logits.shape) != 2:
         _refuse("logits is [rows][vocab]")
-    rows, V = int(logits.shape[0]), int(logits.shape[1])
-    if rows and V > 1 and logits.stride(1) != 1:
+    rows, V = logits.shape
+    ld = logits.stride()
+    if rows and V > 1 and ld[1] != 1:
         _refuse("logits: the values of a row are not side by side")
-    n = 0 if tokens is None else int(tokens.shape[-1])
-    k = 0 if top_ids is None else int(top_ids.shape[-1])
+    n = 0 if tokens is None else tokens.shape[-1]
+    k = 0 if top_ids is None else top_ids.shape[-1]
     if (tokens is None) != (logprob is None) or (top_ids is None) != (top_logprobs is None):
         _refuse("tokens and logprob, top_ids and top_logprobs go together")
-    f32 = lambda x, shape, name: _tensor(x, "float32", shape, name)
-    _op(load_library().hivis_logprobs(C.c_void_p(stream or 0), _dtype(logits.dtype), _ptr(logits), logits.stride(0) if rows > 1 else V, rows, V, C.c_float(temperature),
-                                      _tensor(tokens, "int32", (rows, n), "tokens"), n, f32(logprob, (rows, n), "logprob"), f32(entropy, (rows,), "entropy"), k,
-                                      _tensor(top_ids, "int32", (rows, k), "top_ids"), f32(top_logprobs, (rows, k), "top_logprobs"),
-                                      _tensor(workspace, "uint8", (None,), "workspace"), int(workspace.shape[0])))
+    t = _tensor
+    _op(load_library().hivis_logprobs(stream, _dtype(logits.dtype), logits.data_ptr(), ld[0] if rows > 1 else V, rows, V, temperature, t(tokens, "int32", (rows, n), "tokens"), n,
+                                      t(logprob, "float32", (rows, n), "logprob"), t(entropy, "float32", (rows,), "entropy"), k, t(top_ids, "int32", (rows, k), "top_ids"),
+                                      t(top_logprobs, "float32", (rows, k), "top_logprobs"), t(workspace, "uint8", None, "workspace"), workspace.shape[0]))
 
 
 class Hivis:

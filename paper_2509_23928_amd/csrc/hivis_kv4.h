@@ -249,22 +249,30 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(RowsArgs a) {
 // ---- attention ------------------------------------------------------------------------------------------------------------------------------
 struct Kv4AttnArgs {
     Kv4Dims d; int group, n_seqs, n_rows, max_blocks, tiles; // group: query heads per key head; tiles: row tiles per sequence in the grid
-    float scale2;                                            // softmax scale times log2 e
+    float scale2;                                            // |softmax scale| times log2 e; negative ones negate the queries
+    bool negate;
     const uint8_t* pool; const int *table, *row_start, *kv_len;
     const void* q; long long ldq; const unsigned long long* mask; void* out; long long ldo;
     // rows of the context's passes instead of row_start: m rows of every sequence, row r of sequence s at s * qrows + r in q and s * m + r in out, lengths kv_len[seq0 + s] + len_add
     int m, qrows, seq0, len_add;
+    int chunk, splits; float* ws; int* cnt;                  // key splits: keys each, most per item, partials, arrivals per item (zero between launches)
 };
 
-// A work item is one key head of one sequence and 16 (row, query head) pairs of it, row by row; four wavefronts take 32-key tiles in turn, each with its
-// own running maximum and sum, and merge at the end.
-//   S^T[key][pair] = K Q^T: mfma 16x16x32 with 16 keys as rows.  Lane (n, g) reads a quarter g of key n's codes: one wide load, one scale; products
-//     may take the dims in any order as long as both operands do, so step j multiplies dims g HD/4 + 8j ...
-//   O^T[dim][pair] += V^T P^T: a lane holds the weights of keys 4g.. of both halves as they come out of S^T; V^T comes from a row-major bf16 tile
-//     in LDS through the transposing read.
+// Both kernels multiply alike.  A tile of 16 (row, query head) pairs of one key head, row by row, is the N dimension of
+//   S^T[key][pair] = K Q^T          mfma 16x16x32, 16 keys as rows
+//   O^T[dim][pair] += V^T P^T       a lane's weights of keys 4g .. 4g+3 of two 16-key halves are its operand as they come out of S^T (contractions take any
+//                                   order that both operands share); V^T comes from row-major bf16 in LDS through the transposing read.
 // fp32 queries and weights are split into three bf16 parts (24 bits: exact), so that an fp32 result has fp32 rounding; bf16 queries are one part, their
 // weights are rounded to bf16 (off by at most 2^-8 each, as the result is).
-template <int HD> struct Kv4Tile { static constexpr int VSTRIDE = HD * 2 + 32, BYTES = 32 * VSTRIDE; };
+// Weights are 2^(s - ref); ref follows a pair's largest score s only when that outgrows it by 2^8, so most tiles need no maximum over lanes and no
+// rescaling; sums and maxima are fp32.
+constexpr float KV4_REF0 = -1.0e30f;                         // ref before the first key (finite: a difference of two infinities would be no number)
+constexpr float KV4_SLACK = 8.f;
+constexpr int KV4_MAX_SPLITS = 64;
+
+// LDS rows: the transposing read of four rows, and eight lanes' 16-byte accesses, meet all banks
+template <int HD> constexpr int kv4_vstride() { return HD * 2 + 32; }
+template <int HD> constexpr int kv4_kstride() { return HD * 2 + 16; }
 
 __device__ inline float kv4_xmax(float x) {                  // over the four lanes that share a pair
     const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -278,6 +286,7 @@ __device__ inline float kv4_xsum(float x) {
     const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
+__device__ inline float kv4_nan() { return __uint_as_float(0x7fc00000u); }
 
 // eight codes (one word) as bf16
 __device__ inline kv4_bf16x8 kv4_expand(unsigned w, float scale) {
@@ -295,154 +304,474 @@ __device__ inline void kv4_parts(const float (&x)[8], kv4_bf16x8 (&p)[NP]) {
 #pragma unroll
     for (int k = 0; k < NP; ++k) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) { p[k][e] = (__bf16)rest[e]; rest[e] -= (float)p[k][e]; }
+        for (int e = 0; e < 8; ++e) { p[k][e] = (__bf16)rest[e]; if (k + 1 < NP) rest[e] -= (float)p[k][e]; }
     }
 }
 
-template <typename T, int HD>
-__global__ __launch_bounds__(256) void kv4_attend_kernel(Kv4AttnArgs a) {
-    constexpr int NP = sizeof(T) == 4 ? 3 : 1, STEPS = HD / 32, NB = HD / 16, VSTRIDE = Kv4Tile<HD>::VSTRIDE, NW = 4;
-    constexpr int MSTRIDE = HD + 2;                          // a pair's partial: HD sums, maximum, denominator
-    constexpr int VB = NW * Kv4Tile<HD>::BYTES, MB = NW * 16 * MSTRIDE * 4;
-    __shared__ __align__(16) char lds[VB > MB ? VB : MB];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g = lane >> 4;
-    const int h = blockIdx.x % a.d.heads, ti = blockIdx.x / a.d.heads % a.tiles, s = blockIdx.x / a.d.heads / a.tiles;
-    int row0, orow0, rows, len;
-    if (a.row_start) { row0 = orow0 = a.row_start[s]; rows = a.row_start[s + 1] - row0; len = a.kv_len[s]; }
-    else { row0 = s * a.qrows; orow0 = s * a.m; rows = a.m; len = a.kv_len[a.seq0 + s] + a.len_add; }
-    len = min(len, a.max_blocks << a.d.shift);
-    if (row0 < 0 || rows < 0 || rows > a.n_rows - orow0) return;      // (no rows of this call)
-    const int pairs = rows * a.group, p0 = ti * 16;
-    if (p0 >= pairs) return;
-    // this lane's pair (lanes behind the last repeat it) and the keys it sees: those below `below`, and from `below` on the bits of its mask
-    const int pair = min(p0 + n16, pairs - 1), prow = pair / a.group, ph = h * a.group + pair % a.group;
-    const int below = a.mask ? len - rows : len - rows + prow + 1;
-    const unsigned long long bits = a.mask ? a.mask[orow0 + prow] : 0;
-    const int limit = a.mask ? len : len - rows + min(p0 + 15, pairs - 1) / a.group + 1;       // no pair of the item sees a key from here on
+// four keys of one dim of two 16-key halves, from row-major bf16 rows (row 0 of the tile at `tile`)
+template <int HD>
+__device__ inline kv4_bf16x8 kv4_vfrag(const char* tile, int t, int lane) {
+    typedef __attribute__((address_space(3))) kv4_s16x4* lds_p;
+    const char* src = tile + (4 * (lane >> 4) + (lane & 15) / 4) * kv4_vstride<HD>() + (16 * t + 4 * (lane & 3)) * 2;
+    union { kv4_s16x4 s[2]; kv4_bf16x8 b; } f;
+    f.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_p)src);
+    f.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_p)(src + 16 * kv4_vstride<HD>()));
+    return f.b;
+}
 
-    kv4_bf16x8 qf[STEPS][NP];
-    {
-        const T* q = (const T*)a.q + (long long)(row0 + prow) * a.ldq + (long long)ph * HD + g * (HD / 4);
-#pragma unroll
-        for (int j = 0; j < STEPS; ++j) { float x[8]; kv4_load8<T>(q + 8 * j, x); kv4_parts<NP>(x, qf[j]); }
+// The rows of sequence s: where they start in q and out, how many, how many cached rows
+struct Kv4Seq { int q0, o0, rows, len; };
+__device__ inline Kv4Seq kv4_seq(const Kv4AttnArgs& a, int s) {
+    Kv4Seq x;
+    if (a.row_start) { x.q0 = x.o0 = a.row_start[s]; x.rows = a.row_start[s + 1] - x.q0; x.len = a.kv_len[s]; }
+    else { x.q0 = s * a.qrows; x.o0 = s * a.m; x.rows = a.m; x.len = a.kv_len[a.seq0 + s] + a.len_add; }
+    x.len = min(x.len, a.max_blocks << a.d.shift);
+    if (x.o0 < 0 || x.rows < 0 || x.rows > a.n_rows - x.o0) x.rows = 0;      // (no rows of this call)
+    return x;
+}
+
+// What a lane's pair sees: the keys below `below`, and of the 64 from there on those of `bits`
+struct Kv4Sight {
+    int below; unsigned long long bits;
+    __device__ unsigned long long of(int k0) const {         // of the 64 keys from k0 on, a bit each
+        const int n = below - k0;
+        return (n >= 64 ? ~0ull : (1ull << max(n, 0)) - 1) | (n >= 0 ? n < 64 ? bits << n : 0 : n > -64 ? bits >> -n : 0);
     }
-    kv4_f32x4 o[NB];
+};
+
+// queries of RT tiles of pairs from pair p0 on (lanes behind the last repeat it), in the order of dims that `dim` gives for lane quarter g and step j
+template <typename T, int HD, int RT, int NP, typename Dim>
+__device__ inline void kv4_queries(const Kv4AttnArgs& a, const Kv4Seq& s, int h, int p0, int n16, int g, Dim dim, kv4_bf16x8 (&qf)[RT][HD / 32][NP], Kv4Sight (&see)[RT]) {
+    const int pairs = s.rows * a.group;
 #pragma unroll
-    for (int t = 0; t < NB; ++t) o[t] = kv4_f32x4{0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, l = 0.f;
-    char* const vt = lds + wave * Kv4Tile<HD>::BYTES;
-    const int chunk = kv4_chunk(HD, a.d.block), mask_b = a.d.block - 1;
-    for (int k0 = 32 * wave; k0 < limit; k0 += 32 * NW) {
-        float sc[2][4];
-        unsigned bad_k = 0, bad_v[HD / 32];                  // keys (bits 0..31) whose scale says NaN
+    for (int t = 0; t < RT; ++t) {
+        const int pair = min(p0 + 16 * t + n16, pairs - 1), row = pair / a.group, hq = h * a.group + pair - row * a.group;
+        see[t].below = s.len - s.rows + (a.mask ? 0 : row + 1);
+        see[t].bits = a.mask ? a.mask[s.o0 + row] : 0;
+        const T* q = (const T*)a.q + (long long)(s.q0 + row) * a.ldq + (long long)hq * HD;
 #pragma unroll
-        for (int t = 0; t < HD / 32; ++t) bad_v[t] = 0;
+        for (int j = 0; j < HD / 32; ++j) {
+            float x[8];
+            kv4_load8<T>(q + dim(g, j), x);
+            if (a.negate) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = -x[e];
+            }
+            kv4_parts<NP>(x, qf[t][j]);
+        }
+    }
+}
+
+// One tile of pairs against NH halves of 16 keys: scores x to weights in operand parts; o, ref and l follow.  vis: the keys that the lane's pair sees (bit 16 c + 4 g + r:
+// x[c][r]), unless all do (plain).
+template <int NB, int NH, int NP>
+__device__ inline void kv4_softmax(kv4_f32x4 (&x)[NH], float scale2, bool plain, unsigned long long vis, int g, kv4_f32x4 (&o)[NB], float& ref, float& l, kv4_bf16x8 (&pf)[NH / 2][NP]) {
+    float p[4 * NH];
+    unsigned on[2] = {0, 0};
+    if (!plain) {
+        vis >>= 4 * g;
+        on[0] = (unsigned)vis; on[1] = (unsigned)(vis >> 32);
+#pragma unroll
+        for (int i = 0; i < 4 * NH; ++i)                     // (an all-ones or all-zeros word selects)
+            x[i >> 2][i & 3] = ((int)(on[i >> 3] << (31 - 16 * (i >> 2 & 1) - (i & 3))) >> 31) ? x[i >> 2][i & 3] : -INFINITY;
+    }
+    float mx = x[0][0];
+#pragma unroll
+    for (int i = 1; i < 4 * NH; ++i) mx = fmaxf(mx, x[i >> 2][i & 3]);
+    mx = mx > -INFINITY ? mx * scale2 : -INFINITY;           // (a scale of zero)
+    if (__any(mx > ref + KV4_SLACK)) {
+        const float to = fmaxf(ref, kv4_xmax(mx)), f = __builtin_amdgcn_exp2f(ref - to);
+        ref = to;
+        l *= f;
+#pragma unroll
+        for (int t = 0; t < NB; ++t) o[t] *= f;
+    }
+#pragma unroll
+    for (int i = 0; i < 4 * NH; ++i) p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i >> 2][i & 3], scale2, -ref));
+    if (!plain) {
+#pragma unroll
+        for (int i = 0; i < 4 * NH; ++i) p[i] = ((int)(on[i >> 3] << (31 - 16 * (i >> 2 & 1) - (i & 3))) >> 31) ? p[i] : 0.f;
+    }
+    float s[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { s[i] = p[i] + p[i + 4]; if (NH == 4) s[i] += p[(i + 8) % (4 * NH)] + p[(i + 12) % (4 * NH)]; }
+    l += (s[0] + s[1]) + (s[2] + s[3]);
+#pragma unroll
+    for (int k = 0; k < NH / 2; ++k) {
+        float e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = p[8 * k + i];
+        kv4_parts<NP>(e, pf[k]);
+    }
+}
+// Scales that say NaN never enter the products, where they would reach pairs that do not see the key: a pair that sees one notes which dims of its result are no
+// numbers (a bit per 32; a key's scale: all), and they are set at the end.
+template <int NB>
+__device__ inline void kv4_poison(unsigned no_number, kv4_f32x4 (&o)[NB]) {
+#pragma unroll
+    for (int t = 0; t < NB; ++t) if (no_number >> (t / 2) & 1) o[t] = kv4_f32x4{kv4_nan(), kv4_nan(), kv4_nan(), kv4_nan()};
+}
+
+// result of pair pr (of the sequence), dims c and c + 1
+template <typename T, int HD>
+__device__ inline void kv4_store2(const Kv4AttnArgs& a, const Kv4Seq& s, int h, int pr, int c, float x, float y) {
+    const int row = pr / a.group, hq = h * a.group + pr - row * a.group;
+    T* o = (T*)a.out + (long long)(s.o0 + row) * a.ldo + (long long)hq * HD + c;
+    if constexpr (sizeof(T) == 4) *(float2*)o = make_float2(x, y);
+    else { const kv4_bf16x2 v = {(__bf16)x, (__bf16)y}; *(kv4_bf16x2*)o = v; }
+}
+
+__device__ inline void kv4_put2(float* p, float x, float y) {        // written through, for workgroups of other chiplets
+    __hip_atomic_store((unsigned long long*)p, (unsigned long long)__float_as_uint(y) << 32 | __float_as_uint(x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ inline float2 kv4_get2(const float* p) {
+    const unsigned long long v = __hip_atomic_load((const unsigned long long*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return make_float2(__uint_as_float((unsigned)v), __uint_as_float((unsigned)(v >> 32)));
+}
+
+// ---- few rows: bound by the cache's bytes, or by latency ----
+// A workgroup is one key head of one sequence, 16 RT pairs and a split of `chunk` keys; its four wavefronts take tiles of 32 keys in turn, each with its own
+// ref and sum.  A lane reads a quarter of a key's codes with one wide load and one scale byte, and the next tile's while it multiplies this one;
+// quarters are contiguous, so step j of the products takes dims g HD/4 + 8j of quarter g, and the keys go from registers to the matrix
+// cores.  Values go through the wavefront's own LDS tile (no barrier).  Splits of an item are merged by the workgroup that arrives last.
+template <typename T, int HD, int RT>
+__global__ __launch_bounds__(256, RT * (sizeof(T) == 4 ? 3 : 1) >= 4 ? 1 : 2) void kv4_split_kernel(Kv4AttnArgs a) {
+    constexpr int NP = sizeof(T) == 4 ? 3 : 1, STEPS = HD / 32, NB = HD / 16, VSTRIDE = kv4_vstride<HD>(), NW = 4;
+    constexpr int MSTRIDE = HD + 2;                          // a pair's partial: HD sums, ref, denominator
+    constexpr int VB = NW * 32 * VSTRIDE, MB = NW * 16 * MSTRIDE * 4;
+    __shared__ __align__(16) char lds[VB > MB ? VB : MB];
+    __shared__ int last;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g = lane >> 4;
+    // grid (heads and sequences padded to eights, row tiles, splits): what shares cached rows shares a chiplet and its L2
+    const int sh = blockIdx.x, ti = blockIdx.y, split = blockIdx.z;
+    if (sh >= a.n_seqs * a.d.heads) return;
+    const int seq = sh / a.d.heads, h = sh - seq * a.d.heads;
+    const Kv4Seq s = kv4_seq(a, seq);
+    const int pairs = s.rows * a.group, p0 = ti * 16 * RT;
+    if (p0 >= pairs) return;
+    // keys of the item: no pair of it sees one from `limit` on, all see those below `all`
+    const int limit = a.mask ? s.len : s.len - s.rows + min(p0 + 16 * RT - 1, pairs - 1) / a.group + 1;
+    const int all = s.len - s.rows + (a.mask ? 0 : p0 / a.group + 1);
+    // (more cached rows than the launch was sized for: longer splits)
+    const int chunk = limit > (long long)a.chunk * a.splits ? (int)(((long long)limit + 128ll * a.splits - 1) / (128ll * a.splits)) * 128 : a.chunk;
+    const int splits = max(1, (int)(((long long)limit + chunk - 1) / chunk));
+    if (split >= splits) return;
+    const int end = (int)min((long long)limit, (split + 1ll) * chunk);
+    const int* row = a.table + (size_t)(a.row_start ? seq : a.seq0 + seq) * a.max_blocks;
+    const int bytes = kv4_chunk(HD, a.d.block);
+    char* const vt = lds + wave * 32 * VSTRIDE;
+
+    // this wavefront's blocks, 64 tiles ahead: entry i of lane i
+    int k0 = split * chunk + 32 * wave, e0 = -1, e1 = -1, at = 0;
+    auto entries = [&](int from) {
+        const int key = from + 32 * NW * lane;
+        e0 = key < end ? row[key >> a.d.shift] : -1;
+        e1 = key + 16 < end ? row[(key + 16) >> a.d.shift] : -1;
+    };
+    entries(k0);
+    struct Tile { unsigned k[2][STEPS], v[2][STEPS], kb[2], vb[2]; int e[2]; } now;
+    auto fetch = [&](Tile& t, int key, int i) {
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            const int key = k0 + 16 * half;
-            // the half tile's block; one outside the pool: its keys are left out
-            const int e = key < len ? __builtin_amdgcn_readfirstlane(a.table[(size_t)(a.row_start ? s : a.seq0 + s) * a.max_blocks + (key >> a.d.shift)]) : -1;
-            const bool there = e >= 0 && e < a.d.n_blocks;
-            const uint8_t* c = a.pool + ((size_t)(there ? e : 0) * a.d.heads + h) * chunk;
-            const int r = (key & mask_b) + n16;
-            const bool in = there && key + n16 < len;        // rows behind the last hold anything
-            unsigned kw[STEPS], vw[STEPS];
-#pragma unroll
-            for (int j = 0; j < STEPS; ++j) {
-                kw[j] = ((const unsigned*)(c + r * (HD / 2) + g * (HD / 8)))[j];
-                vw[j] = ((const unsigned*)(c + a.d.block * (HD / 2) + r * (HD / 2) + g * (HD / 8)))[j];
+            const int e = __builtin_amdgcn_readlane(half ? e1 : e0, i);
+            t.e[half] = e;
+            const uint8_t* c = a.pool + ((size_t)(e >= 0 && e < a.d.n_blocks ? e : 0) * a.d.heads + h) * bytes;       // (no block: any one's memory, left out below)
+            const int r = ((key + 16 * half) & (a.d.block - 1)) + n16;
+            const uint8_t *kp = c + r * (HD / 2) + g * (HD / 8), *vp = kp + a.d.block * (HD / 2);
+            if constexpr (HD == 128) {
+                const uint4 x = *(const uint4*)kp, y = *(const uint4*)vp;
+                t.k[half][0] = x.x; t.k[half][1] = x.y; t.k[half][2] = x.z; t.k[half][3] = x.w;
+                t.v[half][0] = y.x; t.v[half][1] = y.y; t.v[half][2] = y.z; t.v[half][3] = y.w;
+            } else {
+                const uint2 x = *(const uint2*)kp, y = *(const uint2*)vp;
+                t.k[half][0] = x.x; t.k[half][1] = x.y; t.v[half][0] = y.x; t.v[half][1] = y.y;
             }
-            unsigned kb = c[a.d.block * HD + r * (HD / 32) + g * (HD / 4) / 32], vb = c[a.d.block * (HD + HD / 32) + r * (HD / 32) + g * (HD / 4) / 32];
-            // a scale that says NaN is taken out of the products, where it would reach rows that do not see the key, and put back below
-            const unsigned long long nk = __ballot(in && kb == 255), nv = __ballot(in && vb == 255);
-            if (nk | nv) {
-                bad_k |= (unsigned)((nk | nk >> 16 | nk >> 32 | nk >> 48) & 0xffff) << (16 * half);
-#pragma unroll
-                for (int t = 0; t < HD / 32; ++t) {          // group t of 32 dims: lanes g = 4 t 32 / HD ..
-                    unsigned long long w = 0;
-#pragma unroll
-                    for (int u = 0; u < 128 / HD; ++u) w |= nv >> (16 * (t * (128 / HD) + u));
-                    bad_v[t] |= (unsigned)(w & 0xffff) << (16 * half);
-                }
-            }
-            if (!in || kb == 255) kb = 127;
-            if (!in || vb == 255) vb = 127;
-            const float ks = __uint_as_float(kb << 23), vs = __uint_as_float(vb << 23);
-            kv4_f32x4 x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int j = 0; j < STEPS; ++j) {
-                const kv4_bf16x8 kf = kv4_expand(kw[j], ks);
-#pragma unroll
-                for (int p = NP - 1; p >= 0; --p) x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[j][p], x, 0, 0, 0);
-                *(kv4_bf16x8*)(vt + (16 * half + n16) * VSTRIDE + (g * (HD / 4) + 8 * j) * 2) = kv4_expand(vw[j], vs);
-            }
-#pragma unroll
-            for (int r4 = 0; r4 < 4; ++r4) {
-                const int kk = key + 4 * g + r4, nw = kk - below;
-                const bool see = there && kk < len && (nw < 0 || (a.mask && nw < 64 && (bits >> nw & 1)));
-                float y = x[r4];
-                if (bad_k >> (16 * half + 4 * g + r4) & 1) y = __uint_as_float(0x7fc00000u);
-                sc[half][r4] = see ? y * a.scale2 : -INFINITY;
-            }
+            const uint8_t* sp = c + a.d.block * HD + r * (HD / 32) + g * (HD / 4) / 32;
+            t.kb[half] = sp[0];
+            t.vb[half] = sp[a.d.block * (HD / 32)];
         }
-        float mx = -INFINITY;
+    };
+    if (k0 < end) fetch(now, k0, 0);
+    kv4_bf16x8 qf[RT][STEPS][NP];
+    Kv4Sight see[RT];
+    kv4_queries<T, HD, RT, NP>(a, s, h, p0, n16, g, [](int g_, int j) { return g_ * (HD / 4) + 8 * j; }, qf, see);
+    kv4_f32x4 o[RT][NB];
+    float ref[RT], l[RT];
+    unsigned no_number[RT];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) mx = fmaxf(mx, sc[i >> 2][i & 3]);
-        const float mn = fmaxf(m, kv4_xmax(mx)), ref = mn == -INFINITY ? 0.f : mn;
-        const float f = __builtin_amdgcn_exp2f(m - ref);
-        m = mn;
-        l *= f;
-        float p[8];
+    for (int t = 0; t < RT; ++t) {
+        ref[t] = KV4_REF0; l[t] = 0.f; no_number[t] = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) { p[i] = __builtin_amdgcn_exp2f(sc[i >> 2][i & 3] - ref); l += p[i]; }
-        kv4_bf16x8 pf[NP];
-        kv4_parts<NP>(p, pf);
-#pragma unroll
-        for (int t = 0; t < NB; ++t) {
-            o[t] *= f;
-            typedef __attribute__((address_space(3))) kv4_s16x4* lds_p;
-            const char* src = vt + (4 * g + n16 / 4) * VSTRIDE + (16 * t + 4 * (n16 & 3)) * 2;
-            union { kv4_s16x4 s[2]; kv4_bf16x8 b; } vf;
-            vf.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_p)(src));
-            vf.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_p)(src + 16 * VSTRIDE));
-#pragma unroll
-            for (int q = NP - 1; q >= 0; --q) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf.b, pf[q], o[t], 0, 0, 0);
-        }
-#pragma unroll
-        for (int t = 0; t < HD / 32; ++t)
-            for (unsigned w = bad_v[t]; w; w &= w - 1) {      // values that are NaN, for the pairs that see them
-                const int kk = k0 + __builtin_ctz(w), nw = kk - below;
-                if (nw < 0 || (a.mask && nw < 64 && (bits >> nw & 1))) { o[2 * t] += __uint_as_float(0x7fc00000u); o[2 * t + 1] += __uint_as_float(0x7fc00000u); }
-            }
+        for (int b = 0; b < NB; ++b) o[t][b] = kv4_f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    l = kv4_xsum(l);
-    __syncthreads();
+    for (; k0 < end; k0 += 32 * NW) {                        // (below 2^31: end is, and a step is short of the next block's last row)
+        Tile t = now;
+        if (++at == 64) { entries(k0 + 32 * NW); at = 0; }
+        if (k0 + 32 * NW < end) fetch(now, k0 + 32 * NW, at);
+        bool plain = k0 + 32 <= all;
+        const bool there0 = t.e[0] >= 0 && t.e[0] < a.d.n_blocks, there1 = t.e[1] >= 0 && t.e[1] < a.d.n_blocks;
+        const bool odd = t.kb[0] == 255 || t.vb[0] == 255 || t.kb[1] == 255 || t.vb[1] == 255;
+        unsigned held = ~0u;                                 // keys that are held
+        if (!plain || !there0 || !there1 || __any(odd)) {
+            plain = false;
+            held = (there0 ? 0xffffu : 0) | (there1 ? 0xffff0000u : 0);
+            if (k0 + 32 > s.len) held &= (1u << (s.len - k0)) - 1;               // (k0 < end <= len)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const bool in = held >> (16 * half + n16) & 1;
+                unsigned long long nk = __ballot(in && t.kb[half] == 255), nv = __ballot(in && t.vb[half] == 255);
+                if (nk | nv)
+                    for (int i = 0; i < 64; ++i) {           // lane i: key i % 16, quarter i / 16
+                        const unsigned dims = nk >> i & 1 ? 15u : nv >> i & 1 ? 1u << ((i >> 4) * (HD / 4) / 32) : 0u;
+                        if (dims)
+#pragma unroll
+                            for (int r = 0; r < RT; ++r) if (see[r].of(k0 + 16 * half + (i & 15)) & 1) no_number[r] |= dims;
+                    }
+                if (!in || t.kb[half] == 255) t.kb[half] = 127;
+                if (!in || t.vb[half] == 255) t.vb[half] = 127;
+            }
+        }
+        kv4_f32x4 x[RT][2];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const float ks = __uint_as_float(t.kb[half] << 23), vs = __uint_as_float(t.vb[half] << 23);
+#pragma unroll
+            for (int j = 0; j < STEPS; ++j) *(kv4_bf16x8*)(vt + (16 * half + n16) * VSTRIDE + (g * (HD / 4) + 8 * j) * 2) = kv4_expand(t.v[half][j], vs);
+#pragma unroll
+            for (int r = 0; r < RT; ++r) x[r][half] = kv4_f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < STEPS; ++j) {
+                const kv4_bf16x8 kf = kv4_expand(t.k[half][j], ks);
+#pragma unroll
+                for (int p = NP - 1; p >= 0; --p)
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) x[r][half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[r][j][p], x[r][half], 0, 0, 0);
+            }
+        }
+        kv4_bf16x8 pf[RT][1][NP];
+#pragma unroll
+        for (int r = 0; r < RT; ++r) kv4_softmax<NB, 2, NP>(x[r], a.scale2, plain, plain ? 0 : see[r].of(k0) & held, g, o[r], ref[r], l[r], pf[r]);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const kv4_bf16x8 vf = kv4_vfrag<HD>(vt, b, lane);
+#pragma unroll
+            for (int p = NP - 1; p >= 0; --p)
+#pragma unroll
+                for (int r = 0; r < RT; ++r) o[r][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[r][0][p], o[r][b], 0, 0, 0);
+        }
+    }
+    // ---- the wavefronts' results, 16 pairs at a time
     float* const mrg = (float*)lds;
-    {
+    const int count = min(16 * RT, pairs - p0), item = sh * a.tiles + ti;
+    constexpr int most = 16 * RT;
+    float* const part = a.ws + ((size_t)item * a.splits) * most * MSTRIDE;       // [split][pair][MSTRIDE]
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        l[r] = kv4_xsum(l[r]);
+        kv4_poison<NB>(no_number[r], o[r]);
+        __syncthreads();
         float* dst = mrg + (wave * 16 + n16) * MSTRIDE;
 #pragma unroll
-        for (int t = 0; t < NB; ++t)
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int r4 = 0; r4 < 4; ++r4) dst[16 * t + 4 * g + r4] = o[t][r4];
-        if (g == 0) { dst[HD] = m; dst[HD + 1] = l; }
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < 16 * HD; i += 256) {
-        const int pr = i / HD, c = i % HD;
-        if (p0 + pr >= pairs) break;
-        float mx = -INFINITY, den = 0.f, num = 0.f;
+            for (int i = 0; i < 2; ++i) *(float2*)(dst + 16 * b + 4 * g + 2 * i) = make_float2(o[r][b][2 * i], o[r][b][2 * i + 1]);
+        if (g == 0) *(float2*)(dst + HD) = make_float2(ref[r], l[r]);
+        __syncthreads();
+        for (int i = threadIdx.x; i < 16 * HD / 2; i += 256) {
+            const int pr = i / (HD / 2), c = 2 * (i % (HD / 2));
+            if (16 * r + pr >= count) break;
+            float mx = KV4_REF0, den = 0.f, n0 = 0.f, n1 = 0.f;
 #pragma unroll
-        for (int w = 0; w < NW; ++w) mx = fmaxf(mx, mrg[(w * 16 + pr) * MSTRIDE + HD]);
-        if (mx == -INFINITY) mx = 0.f;
+            for (int w = 0; w < NW; ++w) mx = fmaxf(mx, mrg[(w * 16 + pr) * MSTRIDE + HD]);
 #pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            const float* src = mrg + (w * 16 + pr) * MSTRIDE;
-            const float f = __builtin_amdgcn_exp2f(src[HD] - mx);
-            den += src[HD + 1] * f; num += src[c] * f;
+            for (int w = 0; w < NW; ++w) {
+                const float* src = mrg + (w * 16 + pr) * MSTRIDE;
+                const float2 st = *(const float2*)(src + HD), v = *(const float2*)(src + c);
+                const float f = __builtin_amdgcn_exp2f(st.x - mx);
+                den += st.y * f; n0 += v.x * f; n1 += v.y * f;
+            }
+            if (splits == 1) {                               // a row that sees nothing: zeros
+                const float inv = den == 0.f ? 0.f : 1.f / den;
+                kv4_store2<T, HD>(a, s, h, p0 + 16 * r + pr, c, n0 * inv, n1 * inv);
+            } else {
+                float* to = part + ((size_t)split * most + 16 * r + pr) * MSTRIDE;
+                kv4_put2(to + c, n0, n1);
+                if (c == 0) kv4_put2(to + HD, mx, den);
+            }
         }
-        const int row = (p0 + pr) / a.group, hq = h * a.group + (p0 + pr) % a.group;
-        const float y = den == 0.f ? 0.f : num / den;        // a row that sees nothing: zero
-        ((T*)a.out)[(long long)(orow0 + row) * a.ldo + (long long)hq * HD + c] = (T)y;
+    }
+    if (splits == 1) return;
+    // ---- arrival: the partials are acknowledged before the count that shows them
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0) last = __hip_atomic_fetch_add(&a.cnt[item], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == splits - 1;
+    __syncthreads();
+    if (!last) return;
+    if (threadIdx.x == 0) __hip_atomic_store(&a.cnt[item], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    // weights of the splits, in their order (the same whoever merges): [pair][split] in LDS, 16 pairs at a time
+    for (int r = 0; r < RT; ++r) {
+        const int np = min(16, count - 16 * r);
+        if (np <= 0) break;
+        __syncthreads();
+        for (int i = threadIdx.x; i < np * splits; i += 256) {
+            const int sp = i / np, pr = i - sp * np;
+            *(float2*)(mrg + 2 * (pr * splits + sp)) = kv4_get2(part + ((size_t)sp * most + 16 * r + pr) * MSTRIDE + HD);
+        }
+        __syncthreads();
+        if ((int)threadIdx.x < np) {
+            float* w = mrg + 2 * threadIdx.x * splits;
+            float mx = KV4_REF0, den = 0.f;
+            for (int sp = 0; sp < splits; ++sp) mx = fmaxf(mx, w[2 * sp]);
+            for (int sp = 0; sp < splits; ++sp) { const float f = __builtin_amdgcn_exp2f(w[2 * sp] - mx); den += w[2 * sp + 1] * f; w[2 * sp] = f; }
+            w[1] = den == 0.f ? 0.f : 1.f / den;
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < np * HD / 2; i += 256) {
+            const int pr = i / (HD / 2), c = 2 * (i % (HD / 2));
+            const float* w = mrg + 2 * pr * splits;
+            const float* from = part + (size_t)(16 * r + pr) * MSTRIDE + c;
+            float n0 = 0.f, n1 = 0.f;
+            for (int sp = 0; sp < splits; sp += 8) {
+                float2 v[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) v[u] = kv4_get2(from + (size_t)min(sp + u, splits - 1) * most * MSTRIDE);
+#pragma unroll
+                for (int u = 0; u < 8; ++u) if (sp + u < splits) { n0 += w[2 * (sp + u)] * v[u].x; n1 += w[2 * (sp + u)] * v[u].y; }
+            }
+            kv4_store2<T, HD>(a, s, h, p0 + 16 * r + pr, c, n0 * w[1], n1 * w[1]);
+        }
+    }
+}
+
+// ---- many rows (prompts): bound by the matrix cores and the vector work of the softmax ----
+// A workgroup is one key head of one sequence and 64 RT pairs, 16 RT per wavefront; the cache is expanded to bf16 once per workgroup, 64 keys at a time, into two
+// LDS buffers in turn (one barrier per tile).  A thread expands a quarter of one key and of one value: one wide load and one scale each, requested
+// a tile ahead.
+template <typename T, int HD, int RT>
+__global__ __launch_bounds__(256, 2) void kv4_rows_kernel(Kv4AttnArgs a) {
+    constexpr int NP = sizeof(T) == 4 ? 3 : 1, STEPS = HD / 32, NB = HD / 16, KT = 64, VSTRIDE = kv4_vstride<HD>(), KSTRIDE = kv4_kstride<HD>();
+    constexpr int BUF = KT * (VSTRIDE + KSTRIDE), NG = HD / 32;
+    extern __shared__ __align__(16) char kv4_lds[];
+    // Bits of a tile's keys: [0] any of the others; [1] not held; [2] the key's scale says NaN; [3 ..] those of the values' groups.  Three tiles in turn: written
+    // before a tile's barrier, read behind it, cleared behind the next one.
+    unsigned long long (*const odd)[3 + NG] = (unsigned long long (*)[3 + NG])(kv4_lds + 2 * BUF);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g = lane >> 4;
+    const int sh = blockIdx.x, ti = a.tiles - 1 - blockIdx.y;                    // (the longest first)
+    if (sh >= a.n_seqs * a.d.heads) return;
+    const int seq = sh / a.d.heads, h = sh - seq * a.d.heads;
+    const Kv4Seq s = kv4_seq(a, seq);
+    const int pairs = s.rows * a.group, p0 = ti * 64 * RT, w0 = p0 + wave * 16 * RT;
+    if (p0 >= pairs) return;
+    const int limit = a.mask ? s.len : s.len - s.rows + min(p0 + 64 * RT - 1, pairs - 1) / a.group + 1;
+    const int mine = w0 >= pairs ? 0 : a.mask ? s.len : s.len - s.rows + min(w0 + 16 * RT - 1, pairs - 1) / a.group + 1;       // of this wavefront
+    const int all = s.len - s.rows + (a.mask ? 0 : w0 / a.group + 1);
+    const int* row = a.table + (size_t)(a.row_start ? seq : a.seq0 + seq) * a.max_blocks;
+    const int bytes = kv4_chunk(HD, a.d.block);
+    if (threadIdx.x < 3 * (3 + NG)) ((unsigned long long*)odd)[threadIdx.x] = 0;
+    __syncthreads();
+
+    const int kr = threadIdx.x >> 2, kq = threadIdx.x & 3;   // this thread's key of a tile and quarter
+    unsigned kc[STEPS], vc[STEPS], kb, vb;
+    bool in;
+    auto entry = [&](int k0) { return k0 + kr < s.len ? row[(k0 + kr) >> a.d.shift] : -1; };
+    int next = entry(0);                                     // block of the tile that is fetched next, a tile ahead of it
+    auto fetch = [&](int k0) {
+        const int key = k0 + kr, e = next;
+        next = entry(k0 + KT);
+        in = e >= 0 && e < a.d.n_blocks;
+        const uint8_t* c = a.pool + ((size_t)(in ? e : 0) * a.d.heads + h) * bytes;
+        const int r = key & (a.d.block - 1);
+        const uint8_t *kp = c + r * (HD / 2) + kq * (HD / 8), *vp = kp + a.d.block * (HD / 2), *sp = c + a.d.block * HD + r * (HD / 32) + kq * (HD / 4) / 32;
+        if constexpr (HD == 128) {
+            const uint4 x = *(const uint4*)kp, y = *(const uint4*)vp;
+            kc[0] = x.x; kc[1] = x.y; kc[2] = x.z; kc[3] = x.w; vc[0] = y.x; vc[1] = y.y; vc[2] = y.z; vc[3] = y.w;
+        } else {
+            const uint2 x = *(const uint2*)kp, y = *(const uint2*)vp;
+            kc[0] = x.x; kc[1] = x.y; vc[0] = y.x; vc[1] = y.y;
+        }
+        kb = sp[0]; vb = sp[a.d.block * (HD / 32)];
+    };
+    fetch(0);
+    kv4_bf16x8 qf[RT][STEPS][NP];
+    Kv4Sight see[RT];
+    kv4_queries<T, HD, RT, NP>(a, s, h, min(w0, pairs - 1), n16, g, [](int g_, int j) { return 32 * j + 8 * g_; }, qf, see);
+    kv4_f32x4 o[RT][NB];
+    float ref[RT], l[RT];
+    unsigned no_number[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        ref[t] = KV4_REF0; l[t] = 0.f; no_number[t] = 0;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) o[t][b] = kv4_f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    int buf = 0, turn = 0;
+    for (int k0 = 0; k0 < limit; k0 += KT, buf ^= 1, turn = turn == 2 ? 0 : turn + 1) {
+        char* const kt = kv4_lds + buf * BUF; char* const vt = kt + KT * KSTRIDE;
+        if (!in || kb == 255 || vb == 255) {
+            const unsigned long long bit = 1ull << kr;
+            atomicOr(&odd[turn][0], bit);
+            atomicOr(&odd[turn][!in ? 1 : kb == 255 ? 2 : 3 + kq * (HD / 4) / 32], bit);
+            if (in && kb == 255 && vb == 255) atomicOr(&odd[turn][3 + kq * (HD / 4) / 32], bit);
+        }
+        const float ks = __uint_as_float((in && kb != 255 ? kb : 127u) << 23), vs = __uint_as_float((in && vb != 255 ? vb : 127u) << 23);
+#pragma unroll
+        for (int j = 0; j < STEPS; ++j) {
+            *(kv4_bf16x8*)(kt + kr * KSTRIDE + (kq * (HD / 4) + 8 * j) * 2) = kv4_expand(kc[j], ks);
+            *(kv4_bf16x8*)(vt + kr * VSTRIDE + (kq * (HD / 4) + 8 * j) * 2) = kv4_expand(vc[j], vs);
+        }
+        __syncthreads();
+        if (k0 + KT < limit) fetch(k0 + KT);
+        if (threadIdx.x < 3 + NG) odd[turn == 0 ? 2 : turn - 1][threadIdx.x] = 0;
+        if (k0 >= mine) continue;
+        kv4_f32x4 x[RT][4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r) x[r][c] = kv4_f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < STEPS; ++j) {
+                const kv4_bf16x8 kf = *(const kv4_bf16x8*)(kt + (16 * c + n16) * KSTRIDE + (32 * j + 8 * g) * 2);
+#pragma unroll
+                for (int p = NP - 1; p >= 0; --p)
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) x[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[r][j][p], x[r][c], 0, 0, 0);
+            }
+        }
+        const bool any = odd[turn][0] != 0, plain = k0 + KT <= all && !any;
+        unsigned long long gone = 0;
+        if (any) {
+            gone = odd[turn][1];
+            for (int b = 0; b <= NG; ++b)
+                for (unsigned long long w = odd[turn][2 + b]; w; w &= w - 1) {
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) if (see[r].of(k0 + __builtin_ctzll(w)) & 1) no_number[r] |= b ? 1u << (b - 1) : 15u;
+                }
+        }
+        kv4_bf16x8 pf[RT][2][NP];
+#pragma unroll
+        for (int r = 0; r < RT; ++r) kv4_softmax<NB, 4, NP>(x[r], a.scale2, plain, plain ? 0 : see[r].of(k0) & ~gone, g, o[r], ref[r], l[r], pf[r]);
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                const kv4_bf16x8 vf = kv4_vfrag<HD>(vt + 32 * k * VSTRIDE, b, lane);
+#pragma unroll
+                for (int p = NP - 1; p >= 0; --p)
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) o[r][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[r][k][p], o[r][b], 0, 0, 0);
+            }
+    }
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        const float den = kv4_xsum(l[r]), inv = den == 0.f ? 0.f : 1.f / den;    // a row that sees nothing: zeros
+        kv4_poison<NB>(no_number[r], o[r]);
+        const int pr = w0 + 16 * r + n16;
+        if (pr < pairs) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int i = 0; i < 4; i += 2) kv4_store2<T, HD>(a, s, h, pr, 16 * b + 4 * g + i, o[r][b][i] * inv, o[r][b][i + 1] * inv);
+        }
     }
 }
 

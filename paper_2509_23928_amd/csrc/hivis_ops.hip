@@ -8,6 +8,7 @@
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
+#include <cstdlib>
 #include <string>
 
 using namespace hivis;
@@ -100,23 +101,62 @@ int kv4_read_launch(hipStream_t st, int type, const RowsArgs& a) {
     return HIVIS_OK;
 }
 
-int kv4_attend_launch(hipStream_t st, int dtype, Kv4AttnArgs a, int max_rows, int max_len, void* ws, long long ws_bytes) {
-    (void)max_len; (void)ws; (void)ws_bytes;
-    a.tiles = (int)(((long long)max_rows * a.group + 15) / 16);
-    const long long wgs = (long long)a.n_seqs * a.tiles * a.d.heads;
-    if (wgs == 0) return HIVIS_OK;
-    if (wgs > 0x7fffffffLL) return op_fail(HIVIS_EINVAL, "%lld work items are more than a launch takes", wgs);
-#define KV4_ATTEND(T_, HD_) hipLaunchKernelGGL((kv4_attend_kernel<T_, HD_>), dim3((unsigned)wgs), dim3(256), 0, st, a)
-    if (dtype == HIVIS_F32) { if (a.d.hd == 128) KV4_ATTEND(float, 128); else KV4_ATTEND(float, 64); }
-    else { if (a.d.hd == 128) KV4_ATTEND(__bf16, 128); else KV4_ATTEND(__bf16, 64); }
-#undef KV4_ATTEND
+// How a call is cut: kernel, pairs per workgroup, keys per split.
+struct Kv4Plan { bool rows; int rt, tiles, chunk, splits; long long items; };
+static Kv4Plan kv4_plan_attend(const Kv4Dims& d, bool f32, int group, int n_seqs, int max_rows, int max_len) {
+    static const int env_rows = getenv("KV4_ROWS") ? atoi(getenv("KV4_ROWS")) : 0, env_rt = getenv("KV4_RT") ? atoi(getenv("KV4_RT")) : 0, env_wgs = getenv("KV4_WGS") ? atoi(getenv("KV4_WGS")) : 0,
+                     env_min = getenv("KV4_MIN") ? atoi(getenv("KV4_MIN")) : 0;
+    const long long pairs = (long long)max_rows * group, sh = (long long)n_seqs * d.heads;
+    Kv4Plan p{};
+    p.rows = env_rows ? pairs >= env_rows : pairs >= 256;
+    if (p.rows) {
+        p.rt = env_rt ? env_rt : !f32 && sh * ((pairs + 127) / 128) >= 512 ? 2 : 1;
+        p.tiles = (int)((pairs + 64 * p.rt - 1) / (64 * p.rt));
+        return p;
+    }
+    p.rt = env_rt ? env_rt : pairs <= 16 ? 1 : pairs <= 32 || f32 ? 2 : 4;
+    p.tiles = (int)((pairs + 16 * p.rt - 1) / (16 * p.rt));
+    p.items = sh * p.tiles;
+    const long long want = env_wgs ? env_wgs : 2048, least = env_min ? env_min : 128;
+    long long chunk = std::max<long long>({least, (p.items * max_len / want + 127) / 128 * 128, ((long long)max_len / KV4_MAX_SPLITS + 128) / 128 * 128});
+    p.chunk = (int)std::min<long long>(chunk, 0x7fffff80);
+    p.splits = std::max(1, (int)(((long long)max_len + p.chunk - 1) / p.chunk));
+    return p;
+}
+static long long kv4_space(const Kv4Plan& p, int hd) {
+    if (p.rows || p.splits == 1) return 16;
+    return (p.items * 4 + 255) / 256 * 256 + p.items * p.splits * 16 * p.rt * (hd + 2) * 4;
+}
+
+int kv4_attend_launch(hipStream_t st, int dtype, Kv4AttnArgs a, int max_rows, int max_len, void* ws) {
+    const bool f32 = dtype == HIVIS_F32;
+    const Kv4Plan p = kv4_plan_attend(a.d, f32, a.group, a.n_seqs, max_rows, max_len);
+    const long long sh = ((long long)a.n_seqs * a.d.heads + 7) / 8 * 8;
+    a.tiles = p.tiles; a.chunk = p.chunk; a.splits = p.splits;
+    a.cnt = (int*)ws; a.ws = (float*)((char*)ws + (p.items * 4 + 255) / 256 * 256);
+#define KV4_ROWS_(T_, HD_, RT_)                                                                                                                               \
+    do {                                                                                                                                                      \
+        constexpr int lds_ = 2 * 64 * (kv4_vstride<HD_>() + kv4_kstride<HD_>()) + 3 * (3 + HD_ / 32) * 8;                                                     \
+        OP_TRY(hipFuncSetAttribute((const void*)kv4_rows_kernel<T_, HD_, RT_>, hipFuncAttributeMaxDynamicSharedMemorySize, lds_));                            \
+        hipLaunchKernelGGL((kv4_rows_kernel<T_, HD_, RT_>), dim3((unsigned)sh, p.tiles), dim3(256), lds_, st, a);                                             \
+    } while (0)
+#define KV4_SPLIT_(T_, HD_, RT_) hipLaunchKernelGGL((kv4_split_kernel<T_, HD_, RT_>), dim3((unsigned)sh, p.tiles, p.splits), dim3(256), 0, st, a)
+#define KV4_FORMS(T_, HD_)                                                                                      \
+    if (p.rows) { if (p.rt == 1) KV4_ROWS_(T_, HD_, 1); else KV4_ROWS_(T_, HD_, 2); }                           \
+    else if (p.rt == 1) KV4_SPLIT_(T_, HD_, 1);                                                                 \
+    else if (p.rt == 2) KV4_SPLIT_(T_, HD_, 2);                                                                 \
+    else KV4_SPLIT_(T_, HD_, 4);
+    if (f32) { if (a.d.hd == 128) { KV4_FORMS(float, 128) } else { KV4_FORMS(float, 64) } }
+    else { if (a.d.hd == 128) { KV4_FORMS(__bf16, 128) } else { KV4_FORMS(__bf16, 64) } }
+#undef KV4_FORMS
+#undef KV4_SPLIT_
+#undef KV4_ROWS_
     OP_TRY(hipGetLastError());
     return HIVIS_OK;
 }
 
-long long kv4_attend_space(const Kv4Dims& d, int n_q_heads, int n_seqs, int max_rows, int max_len) {
-    (void)d; (void)n_q_heads; (void)n_seqs; (void)max_rows; (void)max_len;
-    return 16;
+long long kv4_attend_space(const Kv4Dims& d, int dtype, int n_q_heads, int n_seqs, int max_rows, int max_len) {
+    return kv4_space(kv4_plan_attend(d, dtype == HIVIS_F32, n_q_heads / d.heads, n_seqs, max_rows, max_len), d.hd);
 }
 
 int logprobs_launch(hipStream_t st, int dtype, const LogprobsArgs& a, void* ws, long long ws_bytes) {
@@ -184,14 +224,17 @@ static int check_attention(const hivis_kv4_attention* a, Kv4Dims* d) {
     CHECK(a->dtype == HIVIS_F32 || a->dtype == HIVIS_BF16, "dtype %d unknown", a->dtype);
     CHECK(a->n_q_heads >= 1 && a->n_q_heads % d->heads == 0, "n_q_heads %d is no multiple of n_kv_heads %d", a->n_q_heads, d->heads);
     CHECK(a->n_seqs >= 0 && a->max_rows >= 0 && a->max_len >= 0, "n_seqs %d, max_rows %d, max_len %d", a->n_seqs, a->max_rows, a->max_len);
-    CHECK((long long)a->max_rows * a->n_q_heads <= 0x7fffffffLL / 128, "max_rows %d x n_q_heads %d", a->max_rows, a->n_q_heads);
+    // a launch has at most 2^31 - 1 heads of sequences with their row tiles (of 16 pairs at least), 65535 of those for one head
+    const long long tiles = ((long long)a->max_rows * (a->n_q_heads / d->heads) + 15) / 16;
+    CHECK(tiles <= 65535 && ((long long)a->n_seqs * d->heads + 7) * std::max(tiles, 1LL) <= 0x7fffffffLL, "n_seqs %d, n_kv_heads %d, max_rows %d, n_q_heads %d: more than a launch takes",
+          a->n_seqs, d->heads, a->max_rows, a->n_q_heads);
     return HIVIS_OK;
 }
 
 int64_t hivis_kv4_attend_bytes(const hivis_kv4_attention* a) {
     Kv4Dims d;
     if (int rc = check_attention(a, &d)) return rc;
-    return kv4_attend_space(d, a->n_q_heads, a->n_seqs, a->max_rows, a->max_len);
+    return kv4_attend_space(d, a->dtype, a->n_q_heads, a->n_seqs, a->max_rows, a->max_len);
 }
 
 int hivis_kv4_attend(void* hip_stream, const hivis_kv4_attention* a) {
@@ -208,14 +251,14 @@ int hivis_kv4_attend(void* hip_stream, const hivis_kv4_attention* a) {
           "row strides %lld, %lld: multiples of %d values, of the output not below n_q_heads * head_dim", (long long)a->q_stride, (long long)a->out_stride, align);
     CHECK(a->pool && a->table && a->row_start && a->kv_len && a->q && a->out && a->workspace, "null argument");
     CHECK(aligned(a->pool, 16) && aligned(a->q, 16) && aligned(a->out, 16) && aligned(a->workspace, 16), "pool, q, out and workspace must start at multiples of 16 bytes");
-    const long long need = kv4_attend_space(k.d, a->n_q_heads, a->n_seqs, a->max_rows, a->max_len);
+    const long long need = kv4_attend_space(k.d, a->dtype, a->n_q_heads, a->n_seqs, a->max_rows, a->max_len);
     CHECK(a->workspace_bytes >= need, "workspace of %lld bytes, %lld needed", (long long)a->workspace_bytes, need);
     if (int rc = check_devices({{a->pool, "pool"}, {a->table, "table"}, {a->row_start, "row_start"}, {a->kv_len, "kv_len"}, {a->q, "q"}, {a->mask, "mask"}, {a->out, "out"},
                                 {a->workspace, "workspace"}})) return rc;
-    k.group = a->n_q_heads / k.d.heads; k.n_seqs = a->n_seqs; k.n_rows = a->n_rows; k.max_blocks = a->max_blocks; k.scale2 = (float)(a->scale * 1.4426950408889634);
+    k.group = a->n_q_heads / k.d.heads; k.n_seqs = a->n_seqs; k.n_rows = a->n_rows; k.max_blocks = a->max_blocks; k.scale2 = (float)(std::fabs(a->scale) * 1.4426950408889634); k.negate = a->scale < 0;
     k.pool = (const uint8_t*)a->pool; k.table = a->table; k.row_start = a->row_start; k.kv_len = a->kv_len; k.q = a->q; k.ldq = a->q_stride;
     k.mask = (const unsigned long long*)a->mask; k.out = a->out; k.ldo = a->out_stride;
-    return kv4_attend_launch((hipStream_t)hip_stream, a->dtype, k, a->max_rows, a->max_len, a->workspace, a->workspace_bytes);
+    return kv4_attend_launch((hipStream_t)hip_stream, a->dtype, k, a->max_rows, a->max_len, a->workspace);
 }
 
 static int check_logprobs(int32_t n_rows, int32_t vocab, int32_t top_k) {
