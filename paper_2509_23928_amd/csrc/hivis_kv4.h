@@ -248,14 +248,14 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(RowsArgs a) {
 
 // ---- attention ------------------------------------------------------------------------------------------------------------------------------
 struct Kv4AttnArgs {
-    Kv4Dims d; int group, n_seqs, n_rows, max_blocks, tiles; // group: query heads per key head; tiles: row tiles per sequence in the grid
+    Kv4Dims d; int group, n_seqs, n_rows, max_rows, max_blocks, tiles; // group: query heads per key head; tiles: row tiles per sequence in the grid
     float scale2;                                            // |softmax scale| times log2 e; negative ones negate the queries
     bool negate;
     const uint8_t* pool; const int *table, *row_start, *kv_len;
     const void* q; long long ldq; const unsigned long long* mask; void* out; long long ldo;
     // rows of the context's passes instead of row_start: m rows of every sequence, row r of sequence s at s * qrows + r in q and s * m + r in out, lengths kv_len[seq0 + s] + len_add
     int m, qrows, seq0, len_add;
-    int chunk, splits; float* ws; int* cnt;                  // key splits: keys each, most per item, partials, arrivals per item (zero between launches)
+    float* ws; int* cnt;                                     // kv4_stream_kernel: partials, arrivals per item (zero between launches)
 };
 
 // Both kernels multiply alike.  A tile of 16 (row, query head) pairs of one key head, row by row, is the N dimension of
@@ -268,7 +268,7 @@ struct Kv4AttnArgs {
 // rescaling; sums and maxima are fp32.
 constexpr float KV4_REF0 = -1.0e30f;                         // ref before the first key (finite: a difference of two infinities would be no number)
 constexpr float KV4_SLACK = 8.f;
-constexpr int KV4_MAX_SPLITS = 64;
+constexpr int KV4_UNIT = 128;                                // keys of a unit of work: four wavefronts, 32 each
 
 // LDS rows: the transposing read of four rows, and eight lanes' 16-byte accesses, meet all banks
 template <int HD> constexpr int kv4_vstride() { return HD * 2 + 32; }
@@ -320,13 +320,14 @@ __device__ inline kv4_bf16x8 kv4_vfrag(const char* tile, int t, int lane) {
 }
 
 // The rows of sequence s: where they start in q and out, how many, how many cached rows
-struct Kv4Seq { int q0, o0, rows, len; };
+struct Kv4Seq { int q0, o0, rows, pairs, len; };            // pairs: of the rows that the launch is sized for
 __device__ inline Kv4Seq kv4_seq(const Kv4AttnArgs& a, int s) {
     Kv4Seq x;
     if (a.row_start) { x.q0 = x.o0 = a.row_start[s]; x.rows = a.row_start[s + 1] - x.q0; x.len = a.kv_len[s]; }
     else { x.q0 = s * a.qrows; x.o0 = s * a.m; x.rows = a.m; x.len = a.kv_len[a.seq0 + s] + a.len_add; }
     x.len = min(x.len, a.max_blocks << a.d.shift);
     if (x.o0 < 0 || x.rows < 0 || x.rows > a.n_rows - x.o0) x.rows = 0;      // (no rows of this call)
+    x.pairs = min(x.rows, a.max_rows) * a.group;
     return x;
 }
 
@@ -342,7 +343,7 @@ struct Kv4Sight {
 // queries of RT tiles of pairs from pair p0 on (lanes behind the last repeat it), in the order of dims that `dim` gives for lane quarter g and step j
 template <typename T, int HD, int RT, int NP, typename Dim>
 __device__ inline void kv4_queries(const Kv4AttnArgs& a, const Kv4Seq& s, int h, int p0, int n16, int g, Dim dim, kv4_bf16x8 (&qf)[RT][HD / 32][NP], Kv4Sight (&see)[RT]) {
-    const int pairs = s.rows * a.group;
+    const int pairs = s.pairs;
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
         const int pair = min(p0 + 16 * t + n16, pairs - 1), row = pair / a.group, hq = h * a.group + pair - row * a.group;
@@ -412,63 +413,118 @@ __device__ inline void kv4_poison(unsigned no_number, kv4_f32x4 (&o)[NB]) {
     for (int t = 0; t < NB; ++t) if (no_number >> (t / 2) & 1) o[t] = kv4_f32x4{kv4_nan(), kv4_nan(), kv4_nan(), kv4_nan()};
 }
 
-// result of pair pr (of the sequence), dims c and c + 1
+// result of pair pr (of the sequence), dims c .. c + 3
 template <typename T, int HD>
-__device__ inline void kv4_store2(const Kv4AttnArgs& a, const Kv4Seq& s, int h, int pr, int c, float x, float y) {
+__device__ inline void kv4_store4(const Kv4AttnArgs& a, const Kv4Seq& s, int h, int pr, int c, const kv4_f32x4& x) {
     const int row = pr / a.group, hq = h * a.group + pr - row * a.group;
     T* o = (T*)a.out + (long long)(s.o0 + row) * a.ldo + (long long)hq * HD + c;
-    if constexpr (sizeof(T) == 4) *(float2*)o = make_float2(x, y);
-    else { const kv4_bf16x2 v = {(__bf16)x, (__bf16)y}; *(kv4_bf16x2*)o = v; }
+    if constexpr (sizeof(T) == 4) *(kv4_f32x4*)o = x;
+    else { typedef __bf16 b4 __attribute__((ext_vector_type(4))); *(b4*)o = b4{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]}; }
 }
-
-__device__ inline void kv4_put2(float* p, float x, float y) {        // written through, for workgroups of other chiplets
-    __hip_atomic_store((unsigned long long*)p, (unsigned long long)__float_as_uint(y) << 32 | __float_as_uint(x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ inline float2 kv4_get2(const float* p) {
-    const unsigned long long v = __hip_atomic_load((const unsigned long long*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    return make_float2(__uint_as_float((unsigned)v), __uint_as_float((unsigned)(v >> 32)));
-}
+// Partial results of a workgroup for workgroups of other chiplets: written through, read past the own L2 (agent scope), 16 or 8 bytes at a time
+typedef unsigned kv4_u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned kv4_u32x2 __attribute__((ext_vector_type(2)));
+constexpr int KV4_AGENT = 16;                                // cache policy of buffer accesses: agent scope
+struct Kv4Partials {
+    __amdgpu_buffer_rsrc_t r;
+    __device__ Kv4Partials(float* p, unsigned bytes) : r(__builtin_amdgcn_make_buffer_rsrc(p, 0, bytes, 0x00020000)) {}
+    __device__ void put4(unsigned at, const kv4_f32x4& x) const { __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(kv4_u32x4, x), r, at * 4, 0, KV4_AGENT); }
+    __device__ void put2(unsigned at, float x, float y) const { __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(kv4_u32x2, make_float2(x, y)), r, at * 4, 0, KV4_AGENT); }
+    __device__ kv4_f32x4 get4(unsigned at) const { return __builtin_bit_cast(kv4_f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at * 4, 0, KV4_AGENT)); }
+    __device__ float2 get2(unsigned at) const { return __builtin_bit_cast(float2, __builtin_amdgcn_raw_buffer_load_b64(r, at * 4, 0, KV4_AGENT)); }
+};
 
 // ---- few rows: bound by the cache's bytes, or by latency ----
-// A workgroup is one key head of one sequence, 16 RT pairs and a split of `chunk` keys; its four wavefronts take tiles of 32 keys in turn, each with its own
-// ref and sum.  A lane reads a quarter of a key's codes with one wide load and one scale byte, and the next tile's while it multiplies this one;
-// quarters are contiguous, so step j of the products takes dims g HD/4 + 8j of quarter g, and the keys go from registers to the matrix
-// cores.  Values go through the wavefront's own LDS tile (no barrier).  Splits of an item are merged by the workgroup that arrives last.
+// An item is 16 RT pairs of one key head of one sequence, a unit KV4_UNIT keys of an item; the units of all items in a row are dealt to the workgroups in equal runs, so
+// lengths as different as they come leave no workgroup idle (one workgroup per item and split of a fixed length: 54 us for 48 conversations of 30 to 16000 rows, and 41 with
+// the best length, where most of a grid sized for the longest had nothing to do).  An item that lies in several runs is merged by the workgroup that
+// finishes last.
+// The four wavefronts take tiles of 32 keys in turn, each with its own ref and sum.  A lane reads a quarter of a key's codes with one wide load and one scale byte,
+// and the next tile's while it multiplies this one; quarters are contiguous, so step j of the products takes dims g HD/4 + 8j of quarter g, and the keys
+// go from registers to the matrix cores.  Values go through the wavefront's own LDS tile (no barrier).
+
+// Where the units of the sequences lie in the row of all (fewer than 2^31): 64 sequences at a time, one per lane.  What is the same for all lanes goes to scalar registers.
+__device__ inline int kv4_scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
+// a / b, both the same for all lanes (below 2^22 by a reciprocal, whose quotient is off by one at most: a division by a run-time value is forty dependent instructions)
+__device__ inline int kv4_div(int a, int b) {
+    if (a >= 1 << 22) return kv4_scalar(a / b);
+    int q = kv4_scalar((int)((float)a * __builtin_amdgcn_rcpf((float)b)));
+    const int r = a - q * b;
+    return r < 0 ? q - 1 : r >= b ? q + 1 : q;
+}
+struct Kv4Units {
+    const Kv4AttnArgs& a; int rt, lane, from, before, mine, upto, here;          // sequences from .. from + 63: units before them, of this lane's, up to and with it, of all 64
+    Kv4Seq seq;                                              // this lane's
+    __device__ Kv4Units(const Kv4AttnArgs& a_, int rt_, int lane_) : a(a_), rt(rt_), lane(lane_), from(0), before(0) { load(); }
+    __device__ void load() {
+        seq = kv4_seq(a, min(from + lane, a.n_seqs - 1));
+        mine = from + lane < a.n_seqs ? (seq.pairs + 16 * rt - 1) / (16 * rt) * a.d.heads * blocks(seq.len) : 0;
+        int x = mine;                                        // sums over the lanes below, within rows of 16, then across them
+        x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false); x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+        x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false); x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+        x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false); x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+        upto = x;
+        here = __builtin_amdgcn_readlane(upto, 63);
+    }
+    __device__ void next() { before += here; from += 64; load(); }
+    __device__ static int blocks(int len) { return max(1, (len + KV4_UNIT - 1) / KV4_UNIT); }      // (len: at most 2^31 - 256)
+    __device__ int total() {                                 // of all sequences; stands at the last 64 of them afterwards
+        while (from + 64 < a.n_seqs) next();
+        return before + here;
+    }
+    __device__ int find(int pos, int& base, Kv4Seq& s) {     // the sequence of unit pos (< total()), and its first unit
+        if (pos < before) { from = 0; before = 0; load(); }
+        while (pos >= before + here) next();
+        const int i = __builtin_ctzll(__ballot(pos < before + upto));
+        base = before + __builtin_amdgcn_readlane(upto - mine, i);
+        s.q0 = __builtin_amdgcn_readlane(seq.q0, i); s.o0 = __builtin_amdgcn_readlane(seq.o0, i); s.rows = __builtin_amdgcn_readlane(seq.rows, i);
+        s.pairs = __builtin_amdgcn_readlane(seq.pairs, i); s.len = __builtin_amdgcn_readlane(seq.len, i);
+        return from + i;
+    }
+};
+
+// wavefronts per SIMD that the kernel is compiled for
+template <typename T, int HD, int RT> constexpr int kv4_stream_waves() { return RT == 4 ? 1 : RT == 2 ? sizeof(T) == 4 && HD == 128 ? 1 : 2 : sizeof(T) == 4 && HD == 128 ? 3 : 4; }
 template <typename T, int HD, int RT>
-__global__ __launch_bounds__(256, RT * (sizeof(T) == 4 ? 3 : 1) >= 4 ? 1 : 2) void kv4_split_kernel(Kv4AttnArgs a) {
+__global__ __launch_bounds__(256, (kv4_stream_waves<T, HD, RT>())) void kv4_stream_kernel(Kv4AttnArgs a) {
     constexpr int NP = sizeof(T) == 4 ? 3 : 1, STEPS = HD / 32, NB = HD / 16, VSTRIDE = kv4_vstride<HD>(), NW = 4;
-    constexpr int MSTRIDE = HD + 2;                          // a pair's partial: HD sums, ref, denominator
+    constexpr int MSTRIDE = HD + 4;                          // a pair's results in LDS: HD sums, ref, denominator
     constexpr int VB = NW * 32 * VSTRIDE, MB = NW * 16 * MSTRIDE * 4;
     __shared__ __align__(16) char lds[VB > MB ? VB : MB];
     __shared__ int last;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g = lane >> 4;
-    // grid (heads and sequences padded to eights, row tiles, splits): what shares cached rows shares a chiplet and its L2
-    const int sh = blockIdx.x, ti = blockIdx.y, split = blockIdx.z;
-    if (sh >= a.n_seqs * a.d.heads) return;
-    const int seq = sh / a.d.heads, h = sh - seq * a.d.heads;
-    const Kv4Seq s = kv4_seq(a, seq);
-    const int pairs = s.rows * a.group, p0 = ti * 16 * RT;
-    if (p0 >= pairs) return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    Kv4Units units(a, RT, threadIdx.x & 63);
+    const int total = units.total(), per = kv4_div(total + (int)gridDim.x - 1, gridDim.x);
+    const int bytes = kv4_chunk(HD, a.d.block);
+    char* const vt = lds + wave * 32 * VSTRIDE;
+    const int stop = (int)min((long long)total, (blockIdx.x + 1ll) * per);
+    for (int pos = (int)min((long long)total, (long long)blockIdx.x * per); pos < stop;) {
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));                            // (what follows from it is not kept across items: 80 registers)
+    const int lane = tid & 63, n16 = lane & 15, g = lane >> 4;
+    int base;
+    Kv4Seq s;
+    const int seq = units.find(pos, base, s);
+    const int nb = Kv4Units::blocks(s.len), at_item = kv4_div(pos - base, nb), first = pos - base - at_item * nb;
+    const int ti = a.tiles > 1 ? kv4_div(at_item, a.d.heads) : 0, h = at_item - ti * a.d.heads;
+    const int n_units = min(nb - first, stop - pos), begins = pos - first;       // the item's units here; its first one
+    pos += n_units;
+    const int pairs = s.pairs, p0 = ti * 16 * RT;
     // keys of the item: no pair of it sees one from `limit` on, all see those below `all`
     const int limit = a.mask ? s.len : s.len - s.rows + min(p0 + 16 * RT - 1, pairs - 1) / a.group + 1;
     const int all = s.len - s.rows + (a.mask ? 0 : p0 / a.group + 1);
-    // (more cached rows than the launch was sized for: longer splits)
-    const int chunk = limit > (long long)a.chunk * a.splits ? (int)(((long long)limit + 128ll * a.splits - 1) / (128ll * a.splits)) * 128 : a.chunk;
-    const int splits = max(1, (int)(((long long)limit + chunk - 1) / chunk));
-    if (split >= splits) return;
-    const int end = (int)min((long long)limit, (split + 1ll) * chunk);
+    const int end = (int)min((long long)limit, (long long)(first + n_units) * KV4_UNIT);
     const int* row = a.table + (size_t)(a.row_start ? seq : a.seq0 + seq) * a.max_blocks;
-    const int bytes = kv4_chunk(HD, a.d.block);
-    char* const vt = lds + wave * 32 * VSTRIDE;
 
     // this wavefront's blocks, 64 tiles ahead: entry i of lane i
-    int k0 = split * chunk + 32 * wave, e0 = -1, e1 = -1, at = 0;
+    int k0 = first * KV4_UNIT + 32 * wave, e0 = -1, e1 = -1, at = 0;
     auto entries = [&](int from) {
         const int key = from + 32 * NW * lane;
         e0 = key < end ? row[key >> a.d.shift] : -1;
         e1 = key + 16 < end ? row[(key + 16) >> a.d.shift] : -1;
     };
     entries(k0);
+    const unsigned at_code = n16 * (HD / 2) + g * (HD / 8), at_scale = n16 * (HD / 32) + g * (HD / 4) / 32;
     struct Tile { unsigned k[2][STEPS], v[2][STEPS], kb[2], vb[2]; int e[2]; } now;
     auto fetch = [&](Tile& t, int key, int i) {
 #pragma unroll
@@ -476,8 +532,8 @@ __global__ __launch_bounds__(256, RT * (sizeof(T) == 4 ? 3 : 1) >= 4 ? 1 : 2) vo
             const int e = __builtin_amdgcn_readlane(half ? e1 : e0, i);
             t.e[half] = e;
             const uint8_t* c = a.pool + ((size_t)(e >= 0 && e < a.d.n_blocks ? e : 0) * a.d.heads + h) * bytes;       // (no block: any one's memory, left out below)
-            const int r = ((key + 16 * half) & (a.d.block - 1)) + n16;
-            const uint8_t *kp = c + r * (HD / 2) + g * (HD / 8), *vp = kp + a.d.block * (HD / 2);
+            const int r = (key + 16 * half) & (a.d.block - 1);
+            const uint8_t *kp = c + r * (HD / 2) + at_code, *vp = c + (a.d.block + r) * (HD / 2) + at_code;       // (scalar base, lane's offset)
             if constexpr (HD == 128) {
                 const uint4 x = *(const uint4*)kp, y = *(const uint4*)vp;
                 t.k[half][0] = x.x; t.k[half][1] = x.y; t.k[half][2] = x.z; t.k[half][3] = x.w;
@@ -486,9 +542,8 @@ __global__ __launch_bounds__(256, RT * (sizeof(T) == 4 ? 3 : 1) >= 4 ? 1 : 2) vo
                 const uint2 x = *(const uint2*)kp, y = *(const uint2*)vp;
                 t.k[half][0] = x.x; t.k[half][1] = x.y; t.v[half][0] = y.x; t.v[half][1] = y.y;
             }
-            const uint8_t* sp = c + a.d.block * HD + r * (HD / 32) + g * (HD / 4) / 32;
-            t.kb[half] = sp[0];
-            t.vb[half] = sp[a.d.block * (HD / 32)];
+            t.kb[half] = (c + a.d.block * HD + r * (HD / 32))[at_scale];
+            t.vb[half] = (c + a.d.block * HD + (a.d.block + r) * (HD / 32))[at_scale];
         }
     };
     if (k0 < end) fetch(now, k0, 0);
@@ -560,86 +615,104 @@ __global__ __launch_bounds__(256, RT * (sizeof(T) == 4 ? 3 : 1) >= 4 ? 1 : 2) vo
                 for (int r = 0; r < RT; ++r) o[r][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[r][0][p], o[r][b], 0, 0, 0);
         }
     }
-    // ---- the wavefronts' results, 16 pairs at a time
+    // ---- the wavefronts' results, 16 pairs at a time.  Partials: two places per workgroup, one for an item that began before its run, one for an item that goes
+    // on behind it; a place: [pair][HD] sums, [pair] ref and denominator
+    asm volatile("" : "+v"(tid));
+    const int n16_ = tid & 15, g_ = tid >> 4 & 3;
     float* const mrg = (float*)lds;
-    const int count = min(16 * RT, pairs - p0), item = sh * a.tiles + ti;
-    constexpr int most = 16 * RT;
-    float* const part = a.ws + ((size_t)item * a.splits) * most * MSTRIDE;       // [split][pair][MSTRIDE]
+    const int count = min(16 * RT, pairs - p0);
+    const bool whole = n_units == nb;
+    constexpr int PLACE = 16 * RT * (HD + 2);
+    const Kv4Partials ws(a.ws, gridDim.x * (2u * PLACE * 4));
+    auto place = [&](int wg, bool begins_there) { return (2u * wg + begins_there) * PLACE; };
+    const unsigned part = place(blockIdx.x, first == 0);
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         l[r] = kv4_xsum(l[r]);
         kv4_poison<NB>(no_number[r], o[r]);
         __syncthreads();
-        float* dst = mrg + (wave * 16 + n16) * MSTRIDE;
+        float* dst = mrg + (wave * 16 + n16_) * MSTRIDE;
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) *(float2*)(dst + 16 * b + 4 * g + 2 * i) = make_float2(o[r][b][2 * i], o[r][b][2 * i + 1]);
-        if (g == 0) *(float2*)(dst + HD) = make_float2(ref[r], l[r]);
+        for (int b = 0; b < NB; ++b) *(kv4_f32x4*)(dst + 16 * b + 4 * g_) = o[r][b];
+        if (g_ == 0) *(float2*)(dst + HD) = make_float2(ref[r], l[r]);
         __syncthreads();
-        for (int i = threadIdx.x; i < 16 * HD / 2; i += 256) {
-            const int pr = i / (HD / 2), c = 2 * (i % (HD / 2));
+        for (int i = tid; i < 16 * HD / 4; i += 256) {
+            const int pr = i / (HD / 4), c = 4 * (i % (HD / 4));
             if (16 * r + pr >= count) break;
-            float mx = KV4_REF0, den = 0.f, n0 = 0.f, n1 = 0.f;
+            float mx = KV4_REF0, den = 0.f;
+            kv4_f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int w = 0; w < NW; ++w) mx = fmaxf(mx, mrg[(w * 16 + pr) * MSTRIDE + HD]);
 #pragma unroll
             for (int w = 0; w < NW; ++w) {
                 const float* src = mrg + (w * 16 + pr) * MSTRIDE;
-                const float2 st = *(const float2*)(src + HD), v = *(const float2*)(src + c);
+                const float2 st = *(const float2*)(src + HD);
                 const float f = __builtin_amdgcn_exp2f(st.x - mx);
-                den += st.y * f; n0 += v.x * f; n1 += v.y * f;
+                den += st.y * f; sum += *(const kv4_f32x4*)(src + c) * f;
             }
-            if (splits == 1) {                               // a row that sees nothing: zeros
-                const float inv = den == 0.f ? 0.f : 1.f / den;
-                kv4_store2<T, HD>(a, s, h, p0 + 16 * r + pr, c, n0 * inv, n1 * inv);
-            } else {
-                float* to = part + ((size_t)split * most + 16 * r + pr) * MSTRIDE;
-                kv4_put2(to + c, n0, n1);
-                if (c == 0) kv4_put2(to + HD, mx, den);
+            if (whole) kv4_store4<T, HD>(a, s, h, p0 + 16 * r + pr, c, sum * (den == 0.f ? 0.f : 1.f / den));         // (a row that sees nothing: zeros)
+            else {
+                ws.put4(part + (16 * r + pr) * HD + c, sum);
+                if (c == 0) ws.put2(part + 16 * RT * HD + 2 * (16 * r + pr), mx, den);
             }
         }
     }
-    if (splits == 1) return;
+    __syncthreads();                                         // (the next item's values go where these results were)
+    if (whole) continue;
     // ---- arrival: the partials are acknowledged before the count that shows them
+    const int w0 = kv4_div(begins, per), parts = kv4_div(begins + nb - 1, per) - w0 + 1, item = (seq * a.tiles + ti) * a.d.heads + h;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (threadIdx.x == 0) last = __hip_atomic_fetch_add(&a.cnt[item], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == splits - 1;
+    if (tid == 0) last = __hip_atomic_fetch_add(&a.cnt[item], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == parts - 1;
     __syncthreads();
-    if (!last) return;
-    if (threadIdx.x == 0) __hip_atomic_store(&a.cnt[item], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    // weights of the splits, in their order (the same whoever merges): [pair][split] in LDS, 16 pairs at a time
-    for (int r = 0; r < RT; ++r) {
-        const int np = min(16, count - 16 * r);
-        if (np <= 0) break;
-        __syncthreads();
-        for (int i = threadIdx.x; i < np * splits; i += 256) {
-            const int sp = i / np, pr = i - sp * np;
-            *(float2*)(mrg + 2 * (pr * splits + sp)) = kv4_get2(part + ((size_t)sp * most + 16 * r + pr) * MSTRIDE + HD);
-        }
-        __syncthreads();
-        if ((int)threadIdx.x < np) {
-            float* w = mrg + 2 * threadIdx.x * splits;
-            float mx = KV4_REF0, den = 0.f;
-            for (int sp = 0; sp < splits; ++sp) mx = fmaxf(mx, w[2 * sp]);
-            for (int sp = 0; sp < splits; ++sp) { const float f = __builtin_amdgcn_exp2f(w[2 * sp] - mx); den += w[2 * sp + 1] * f; w[2 * sp] = f; }
-            w[1] = den == 0.f ? 0.f : 1.f / den;
-        }
-        __syncthreads();
-        for (int i = threadIdx.x; i < np * HD / 2; i += 256) {
-            const int pr = i / (HD / 2), c = 2 * (i % (HD / 2));
-            const float* w = mrg + 2 * pr * splits;
-            const float* from = part + (size_t)(16 * r + pr) * MSTRIDE + c;
-            float n0 = 0.f, n1 = 0.f;
-            for (int sp = 0; sp < splits; sp += 8) {
-                float2 v[8];
+    if (!last) continue;
+    if (tid == 0) __hip_atomic_store(&a.cnt[item], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    // Merge, in the order of the keys (the same whoever merges): a thread takes four dims of a pair and eight partials at a time, all requested at once with their
+    // refs and denominators; where there are fewer pairs than threads for them, several threads share the partials and add up in LDS.
+    int sh_pr = 0;                                           // pairs padded to a power of two
+    while ((1 << sh_pr) < count) ++sh_pr;
+    const int elems = HD / 4 << sh_pr, groups = max(1, 256 / elems);
+    for (int e = tid; e < max(256, elems); e += 256) {
+        const int el = e & (elems - 1), grp = elems < 256 ? e / elems : 0, pr = min(el / (HD / 4), count - 1), c = 4 * (el % (HD / 4));
+        float mx = KV4_REF0, den = 0.f;
+        kv4_f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+        for (int q0 = grp; q0 < parts; q0 += 8 * groups) {
+            kv4_f32x4 v[8];
+            float2 st[8];
 #pragma unroll
-                for (int u = 0; u < 8; ++u) v[u] = kv4_get2(from + (size_t)min(sp + u, splits - 1) * most * MSTRIDE);
-#pragma unroll
-                for (int u = 0; u < 8; ++u) if (sp + u < splits) { n0 += w[2 * (sp + u)] * v[u].x; n1 += w[2 * (sp + u)] * v[u].y; }
+            for (int u = 0; u < 8; ++u) {
+                const int q = min(q0 + u * groups, parts - 1);
+                const unsigned from = place(w0 + q, q == 0);
+                v[u] = ws.get4(from + pr * HD + c); st[u] = ws.get2(from + 16 * RT * HD + 2 * pr);
             }
-            kv4_store2<T, HD>(a, s, h, p0 + 16 * r + pr, c, n0 * w[1], n1 * w[1]);
+            float to = mx;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) { if (q0 + u * groups >= parts) st[u] = make_float2(KV4_REF0, 0.f); to = fmaxf(to, st[u].x); }
+            const float f = __builtin_amdgcn_exp2f(mx - to);
+            den *= f; sum *= f; mx = to;
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                if (q0 + u * groups < parts) { const float w = __builtin_amdgcn_exp2f(st[u].x - to); den += st[u].y * w; sum += v[u] * w; }
         }
+        if (groups > 1) {
+            float* at = mrg + e * 6;                         // (256 of them)
+            at[0] = mx; at[1] = den;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) at[2 + i] = sum[i];
+            __syncthreads();
+            if (grp == 0) {
+                for (int u = 1; u < groups; ++u) {
+                    const float* o = mrg + (u * elems + el) * 6;
+                    const float to = fmaxf(mx, o[0]), f = __builtin_amdgcn_exp2f(mx - to), w = __builtin_amdgcn_exp2f(o[0] - to);
+                    den = den * f + o[1] * w; mx = to;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sum[i] = sum[i] * f + o[2 + i] * w;
+                }
+            }
+        }
+        if (grp == 0 && el / (HD / 4) < count) kv4_store4<T, HD>(a, s, h, p0 + pr, c, sum * (den == 0.f ? 0.f : 1.f / den));
+    }
+    __syncthreads();
     }
 }
 
@@ -660,7 +733,7 @@ __global__ __launch_bounds__(256, 2) void kv4_rows_kernel(Kv4AttnArgs a) {
     if (sh >= a.n_seqs * a.d.heads) return;
     const int seq = sh / a.d.heads, h = sh - seq * a.d.heads;
     const Kv4Seq s = kv4_seq(a, seq);
-    const int pairs = s.rows * a.group, p0 = ti * 64 * RT, w0 = p0 + wave * 16 * RT;
+    const int pairs = s.pairs, p0 = ti * 64 * RT, w0 = p0 + wave * 16 * RT;
     if (p0 >= pairs) return;
     const int limit = a.mask ? s.len : s.len - s.rows + min(p0 + 64 * RT - 1, pairs - 1) / a.group + 1;
     const int mine = w0 >= pairs ? 0 : a.mask ? s.len : s.len - s.rows + min(w0 + 16 * RT - 1, pairs - 1) / a.group + 1;       // of this wavefront
@@ -769,8 +842,7 @@ __global__ __launch_bounds__(256, 2) void kv4_rows_kernel(Kv4AttnArgs a) {
         if (pr < pairs) {
 #pragma unroll
             for (int b = 0; b < NB; ++b)
-#pragma unroll
-                for (int i = 0; i < 4; i += 2) kv4_store2<T, HD>(a, s, h, pr, 16 * b + 4 * g + i, o[r][b][i] * inv, o[r][b][i + 1] * inv);
+                kv4_store4<T, HD>(a, s, h, pr, 16 * b + 4 * g, o[r][b] * inv);
         }
     }
 }

@@ -101,11 +101,10 @@ int kv4_read_launch(hipStream_t st, int type, const RowsArgs& a) {
     return HIVIS_OK;
 }
 
-// How a call is cut: kernel, pairs per workgroup, keys per split.
-struct Kv4Plan { bool rows; int rt, tiles, chunk, splits; long long items; };
+// How a call is cut: kernel, pairs per workgroup or item, row tiles of a sequence at most, workgroups.
+struct Kv4Plan { bool rows; int rt, tiles, wgs; long long items; };
 static Kv4Plan kv4_plan_attend(const Kv4Dims& d, bool f32, int group, int n_seqs, int max_rows, int max_len) {
-    static const int env_rows = getenv("KV4_ROWS") ? atoi(getenv("KV4_ROWS")) : 0, env_rt = getenv("KV4_RT") ? atoi(getenv("KV4_RT")) : 0, env_wgs = getenv("KV4_WGS") ? atoi(getenv("KV4_WGS")) : 0,
-                     env_min = getenv("KV4_MIN") ? atoi(getenv("KV4_MIN")) : 0;
+    static const int env_rows = getenv("KV4_ROWS") ? atoi(getenv("KV4_ROWS")) : 0, env_rt = getenv("KV4_RT") ? atoi(getenv("KV4_RT")) : 0, env_wgs = getenv("KV4_WGS") ? atoi(getenv("KV4_WGS")) : 0;
     const long long pairs = (long long)max_rows * group, sh = (long long)n_seqs * d.heads;
     Kv4Plan p{};
     p.rows = env_rows ? pairs >= env_rows : pairs >= 256;
@@ -117,39 +116,34 @@ static Kv4Plan kv4_plan_attend(const Kv4Dims& d, bool f32, int group, int n_seqs
     p.rt = env_rt ? env_rt : pairs <= 16 ? 1 : pairs <= 32 || f32 ? 2 : 4;
     p.tiles = (int)((pairs + 16 * p.rt - 1) / (16 * p.rt));
     p.items = sh * p.tiles;
-    const long long want = env_wgs ? env_wgs : 2048, least = env_min ? env_min : 128;
-    long long chunk = std::max<long long>({least, (p.items * max_len / want + 127) / 128 * 128, ((long long)max_len / KV4_MAX_SPLITS + 128) / 128 * 128});
-    p.chunk = (int)std::min<long long>(chunk, 0x7fffff80);
-    p.splits = std::max(1, (int)(((long long)max_len + p.chunk - 1) / p.chunk));
+    const long long most = env_wgs ? env_wgs : f32 ? 512 : 1024;
+    p.wgs = (int)std::min<long long>(most, p.items * std::max(1, (max_len + KV4_UNIT - 1) / KV4_UNIT));
     return p;
 }
-static long long kv4_space(const Kv4Plan& p, int hd) {
-    if (p.rows || p.splits == 1) return 16;
-    return (p.items * 4 + 255) / 256 * 256 + p.items * p.splits * 16 * p.rt * (hd + 2) * 4;
-}
+static long long kv4_counters(const Kv4Plan& p) { return (p.items * 4 + 255) / 256 * 256; }
+static long long kv4_space(const Kv4Plan& p, int hd) { return p.rows ? 16 : kv4_counters(p) + 2LL * p.wgs * 16 * p.rt * (hd + 2) * 4; }
 
 int kv4_attend_launch(hipStream_t st, int dtype, Kv4AttnArgs a, int max_rows, int max_len, void* ws) {
     const bool f32 = dtype == HIVIS_F32;
     const Kv4Plan p = kv4_plan_attend(a.d, f32, a.group, a.n_seqs, max_rows, max_len);
     const long long sh = ((long long)a.n_seqs * a.d.heads + 7) / 8 * 8;
-    a.tiles = p.tiles; a.chunk = p.chunk; a.splits = p.splits;
-    a.cnt = (int*)ws; a.ws = (float*)((char*)ws + (p.items * 4 + 255) / 256 * 256);
+    a.tiles = p.tiles; a.max_rows = max_rows; a.cnt = (int*)ws; a.ws = (float*)((char*)ws + kv4_counters(p));
 #define KV4_ROWS_(T_, HD_, RT_)                                                                                                                               \
     do {                                                                                                                                                      \
         constexpr int lds_ = 2 * 64 * (kv4_vstride<HD_>() + kv4_kstride<HD_>()) + 3 * (3 + HD_ / 32) * 8;                                                     \
         OP_TRY(hipFuncSetAttribute((const void*)kv4_rows_kernel<T_, HD_, RT_>, hipFuncAttributeMaxDynamicSharedMemorySize, lds_));                            \
         hipLaunchKernelGGL((kv4_rows_kernel<T_, HD_, RT_>), dim3((unsigned)sh, p.tiles), dim3(256), lds_, st, a);                                             \
     } while (0)
-#define KV4_SPLIT_(T_, HD_, RT_) hipLaunchKernelGGL((kv4_split_kernel<T_, HD_, RT_>), dim3((unsigned)sh, p.tiles, p.splits), dim3(256), 0, st, a)
+#define KV4_STREAM_(T_, HD_, RT_) hipLaunchKernelGGL((kv4_stream_kernel<T_, HD_, RT_>), dim3(p.wgs), dim3(256), 0, st, a)
 #define KV4_FORMS(T_, HD_)                                                                                      \
     if (p.rows) { if (p.rt == 1) KV4_ROWS_(T_, HD_, 1); else KV4_ROWS_(T_, HD_, 2); }                           \
-    else if (p.rt == 1) KV4_SPLIT_(T_, HD_, 1);                                                                 \
-    else if (p.rt == 2) KV4_SPLIT_(T_, HD_, 2);                                                                 \
-    else KV4_SPLIT_(T_, HD_, 4);
+    else if (p.rt == 1) KV4_STREAM_(T_, HD_, 1);                                                                 \
+    else if (p.rt == 2) KV4_STREAM_(T_, HD_, 2);                                                                 \
+    else KV4_STREAM_(T_, HD_, 4);
     if (f32) { if (a.d.hd == 128) { KV4_FORMS(float, 128) } else { KV4_FORMS(float, 64) } }
     else { if (a.d.hd == 128) { KV4_FORMS(__bf16, 128) } else { KV4_FORMS(__bf16, 64) } }
 #undef KV4_FORMS
-#undef KV4_SPLIT_
+#undef KV4_STREAM_
 #undef KV4_ROWS_
     OP_TRY(hipGetLastError());
     return HIVIS_OK;
@@ -242,7 +236,9 @@ int hivis_kv4_attend(void* hip_stream, const hivis_kv4_attention* a) {
     if (int rc = check_attention(a, &k.d)) return rc;
     CHECK(a->n_rows >= 0 && (long long)a->n_rows * a->n_q_heads <= 0x7fffffffLL, "n_rows %d x n_q_heads %d", a->n_rows, a->n_q_heads);
     if (a->n_seqs == 0 || a->max_rows == 0 || a->n_rows == 0) return HIVIS_OK;
-    CHECK(a->max_blocks >= 1 && (long long)a->max_blocks * k.d.block <= 0x7fffffffLL, "max_blocks %d: a sequence's positions must be in 0..2^31-1", a->max_blocks);
+    CHECK(a->max_blocks >= 1 && (long long)a->max_blocks * k.d.block <= 0x7fffffffLL - 255, "max_blocks %d: a sequence's positions must be below 2^31 - 256", a->max_blocks);
+    CHECK((double)a->n_seqs * k.d.heads * (((long long)a->max_rows * (a->n_q_heads / k.d.heads) + 15) / 16) * ((long long)a->max_blocks * k.d.block / KV4_UNIT + 1) < 2147483648.0,
+          "n_seqs %d, max_blocks %d, max_rows %d: more than a launch takes", a->n_seqs, a->max_blocks, a->max_rows);
     CHECK(!a->mask || a->max_rows <= 64, "max_rows %d: a mask has bits for 64 rows", a->max_rows);
     CHECK(std::isfinite(a->scale), "scale is not finite");
     const int align = a->dtype == HIVIS_F32 ? 4 : 8;
