@@ -15,6 +15,8 @@ typedef __bf16 kv4_bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 kv4_bf16x8 __attribute__((ext_vector_type(8)));
 typedef float kv4_f32x4 __attribute__((ext_vector_type(4)));
 typedef short kv4_s16x4 __attribute__((ext_vector_type(4)));
+typedef unsigned kv4_u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned kv4_u32x2 __attribute__((ext_vector_type(2)));
 
 // What the kernels know of a cache
 struct Kv4Dims { int heads, hd, block, shift, n_blocks; };       // block = 1 << shift rows
@@ -269,6 +271,9 @@ struct Kv4AttnArgs {
 constexpr float KV4_REF0 = -1.0e30f;                         // ref before the first key (finite: a difference of two infinities would be no number)
 constexpr float KV4_SLACK = 8.f;
 constexpr int KV4_UNIT = 128;                                // keys of a unit of work: four wavefronts, 32 each
+#ifndef KV4_ITEM_COST
+constexpr int KV4_ITEM_COST = 2;
+#endif
 
 // LDS rows: the transposing read of four rows, and eight lanes' 16-byte accesses, meet all banks
 template <int HD> constexpr int kv4_vstride() { return HD * 2 + 32; }
@@ -285,6 +290,12 @@ __device__ inline float kv4_xsum(float x) {
     x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
     const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+// orders LDS accesses only (__syncthreads waits for all requests to memory as well)
+__device__ inline void kv4_lds_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 __device__ inline float kv4_nan() { return __uint_as_float(0x7fc00000u); }
 
@@ -340,27 +351,38 @@ struct Kv4Sight {
     }
 };
 
-// queries of RT tiles of pairs from pair p0 on (lanes behind the last repeat it), in the order of dims that `dim` gives for lane quarter g and step j
-template <typename T, int HD, int RT, int NP, typename Dim>
-__device__ inline void kv4_queries(const Kv4AttnArgs& a, const Kv4Seq& s, int h, int p0, int n16, int g, Dim dim, kv4_bf16x8 (&qf)[RT][HD / 32][NP], Kv4Sight (&see)[RT]) {
-    const int pairs = s.pairs;
+// Queries of RT tiles of pairs from pair p0 on (lanes behind the last repeat it), eight values of each in the order of dims that `dim` gives for lane quarter g and
+// step j: as they lie in memory, and as operand parts
+template <typename T> struct Kv4Raw { kv4_u32x4 x[sizeof(T) / 2]; };
+template <typename T, int HD, int RT, typename Dim>
+__device__ inline void kv4_queries(const Kv4AttnArgs& a, const Kv4Seq& s, int h, int p0, int n16, int g, Dim dim, Kv4Raw<T> (&raw)[RT][HD / 32], Kv4Sight (&see)[RT]) {
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-        const int pair = min(p0 + 16 * t + n16, pairs - 1), row = pair / a.group, hq = h * a.group + pair - row * a.group;
+        const int pair = min(p0 + 16 * t + n16, s.pairs - 1), row = a.group == 1 ? pair : pair / a.group, hq = h * a.group + pair - row * a.group;
         see[t].below = s.len - s.rows + (a.mask ? 0 : row + 1);
         see[t].bits = a.mask ? a.mask[s.o0 + row] : 0;
         const T* q = (const T*)a.q + (long long)(s.q0 + row) * a.ldq + (long long)hq * HD;
 #pragma unroll
-        for (int j = 0; j < HD / 32; ++j) {
-            float x[8];
-            kv4_load8<T>(q + dim(g, j), x);
-            if (a.negate) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = -x[e];
-            }
-            kv4_parts<NP>(x, qf[t][j]);
-        }
+        for (int j = 0; j < HD / 32; ++j) raw[t][j] = *(const Kv4Raw<T>*)(q + dim(g, j));
     }
+}
+template <typename T, int HD, int RT, int NP>
+__device__ inline void kv4_query_parts(const Kv4AttnArgs& a, const Kv4Raw<T> (&raw)[RT][HD / 32], kv4_bf16x8 (&qf)[RT][HD / 32][NP]) {
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+        for (int j = 0; j < HD / 32; ++j) {
+            if constexpr (sizeof(T) == 2) {
+                kv4_u32x4 x = raw[t][j].x[0];
+                if (a.negate) x ^= 0x80008000u;
+                qf[t][j][0] = __builtin_bit_cast(kv4_bf16x8, x);
+            } else {
+                float x[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) { x[e] = __uint_as_float(raw[t][j].x[e >> 2][e & 3]); if (a.negate) x[e] = -x[e]; }
+                kv4_parts<NP>(x, qf[t][j]);
+            }
+        }
 }
 
 // One tile of pairs against NH halves of 16 keys: scores x to weights in operand parts; o, ref and l follow.  vis: the keys that the lane's pair sees (bit 16 c + 4 g + r:
@@ -422,8 +444,6 @@ __device__ inline void kv4_store4(const Kv4AttnArgs& a, const Kv4Seq& s, int h, 
     else { typedef __bf16 b4 __attribute__((ext_vector_type(4))); *(b4*)o = b4{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]}; }
 }
 // Partial results of a workgroup for workgroups of other chiplets: written through, read past the own L2 (agent scope), 16 or 8 bytes at a time
-typedef unsigned kv4_u32x4 __attribute__((ext_vector_type(4)));
-typedef unsigned kv4_u32x2 __attribute__((ext_vector_type(2)));
 constexpr int KV4_AGENT = 16;                                // cache policy of buffer accesses: agent scope
 struct Kv4Partials {
     __amdgpu_buffer_rsrc_t r;
@@ -458,7 +478,7 @@ struct Kv4Units {
     __device__ Kv4Units(const Kv4AttnArgs& a_, int rt_, int lane_) : a(a_), rt(rt_), lane(lane_), from(0), before(0) { load(); }
     __device__ void load() {
         seq = kv4_seq(a, min(from + lane, a.n_seqs - 1));
-        mine = from + lane < a.n_seqs ? (seq.pairs + 16 * rt - 1) / (16 * rt) * a.d.heads * blocks(seq.len) : 0;
+        mine = from + lane < a.n_seqs ? (seq.pairs + 16 * rt - 1) / (16 * rt) * a.d.heads * (blocks(seq.len) + KV4_ITEM_COST) : 0;
         int x = mine;                                        // sums over the lanes below, within rows of 16, then across them
         x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false); x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
         x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false); x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
@@ -484,12 +504,12 @@ struct Kv4Units {
 };
 
 // wavefronts per SIMD that the kernel is compiled for
-template <typename T, int HD, int RT> constexpr int kv4_stream_waves() { return RT == 4 ? 1 : RT == 2 ? sizeof(T) == 4 && HD == 128 ? 1 : 2 : sizeof(T) == 4 && HD == 128 ? 3 : 4; }
+template <typename T, int HD, int RT> constexpr int kv4_stream_waves() { return RT == 4 ? 1 : RT == 2 ? sizeof(T) == 4 && HD == 128 ? 1 : 2 : HD == 128 ? sizeof(T) == 4 ? 2 : 3 : sizeof(T) == 4 ? 3 : 4; }
 template <typename T, int HD, int RT>
 __global__ __launch_bounds__(256, (kv4_stream_waves<T, HD, RT>())) void kv4_stream_kernel(Kv4AttnArgs a) {
     constexpr int NP = sizeof(T) == 4 ? 3 : 1, STEPS = HD / 32, NB = HD / 16, VSTRIDE = kv4_vstride<HD>(), NW = 4;
     constexpr int MSTRIDE = HD + 4;                          // a pair's results in LDS: HD sums, ref, denominator
-    constexpr int VB = NW * 32 * VSTRIDE, MB = NW * 16 * MSTRIDE * 4;
+    constexpr int VB = NW * 32 * VSTRIDE, MB = NW * 16 * MSTRIDE * 4, PLACE = 16 * RT * (HD + 2);
     __shared__ __align__(16) char lds[VB > MB ? VB : MB];
     __shared__ int last;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -497,41 +517,32 @@ __global__ __launch_bounds__(256, (kv4_stream_waves<T, HD, RT>())) void kv4_stre
     const int total = units.total(), per = kv4_div(total + (int)gridDim.x - 1, gridDim.x);
     const int bytes = kv4_chunk(HD, a.d.block);
     char* const vt = lds + wave * 32 * VSTRIDE;
+    float* const mrg = (float*)lds;
     const int stop = (int)min((long long)total, (blockIdx.x + 1ll) * per);
-    for (int pos = (int)min((long long)total, (long long)blockIdx.x * per); pos < stop;) {
-    int tid = threadIdx.x;
-    asm volatile("" : "+v"(tid));                            // (what follows from it is not kept across items: 80 registers)
-    const int lane = tid & 63, n16 = lane & 15, g = lane >> 4;
-    int base;
-    Kv4Seq s;
-    const int seq = units.find(pos, base, s);
-    const int nb = Kv4Units::blocks(s.len), at_item = kv4_div(pos - base, nb), first = pos - base - at_item * nb;
-    const int ti = a.tiles > 1 ? kv4_div(at_item, a.d.heads) : 0, h = at_item - ti * a.d.heads;
-    const int n_units = min(nb - first, stop - pos), begins = pos - first;       // the item's units here; its first one
-    pos += n_units;
-    const int pairs = s.pairs, p0 = ti * 16 * RT;
-    // keys of the item: no pair of it sees one from `limit` on, all see those below `all`
-    const int limit = a.mask ? s.len : s.len - s.rows + min(p0 + 16 * RT - 1, pairs - 1) / a.group + 1;
-    const int all = s.len - s.rows + (a.mask ? 0 : p0 / a.group + 1);
-    const int end = (int)min((long long)limit, (long long)(first + n_units) * KV4_UNIT);
-    const int* row = a.table + (size_t)(a.row_start ? seq : a.seq0 + seq) * a.max_blocks;
+    int pos = (int)min((long long)total, (long long)blockIdx.x * per);
+    if (pos >= stop) return;
+    // Partials: two places per workgroup, [0] for an item that began before its run, [1] for an item that goes on behind it; a place: [pair][HD] sums, [pair] ref and denominator
+    const Kv4Partials ws(a.ws, gridDim.x * (2u * PLACE * 4));
+    auto place = [&](int wg, bool begins_there) { return (2u * wg + begins_there) * PLACE; };
 
-    // this wavefront's blocks, 64 tiles ahead: entry i of lane i
-    int k0 = first * KV4_UNIT + 32 * wave, e0 = -1, e1 = -1, at = 0;
-    auto entries = [&](int from) {
+    // ---- an item's part in this run: what it is, and the first requests to memory
+    struct Item { Kv4Seq s; int seq, ti, h, nb, first, units, begins; } it;
+    struct Tile { unsigned k[2][STEPS], v[2][STEPS], kb[2], vb[2]; int e[2]; } now;
+    Kv4Raw<T> raw[RT][STEPS];
+    Kv4Sight see[RT];
+    int k0, end, all, e0, e1, at;
+    const int* row;
+    auto entries = [&](int from, int lane) {                 // this wavefront's blocks, 64 tiles ahead: entry i of lane i
         const int key = from + 32 * NW * lane;
         e0 = key < end ? row[key >> a.d.shift] : -1;
         e1 = key + 16 < end ? row[(key + 16) >> a.d.shift] : -1;
     };
-    entries(k0);
-    const unsigned at_code = n16 * (HD / 2) + g * (HD / 8), at_scale = n16 * (HD / 32) + g * (HD / 4) / 32;
-    struct Tile { unsigned k[2][STEPS], v[2][STEPS], kb[2], vb[2]; int e[2]; } now;
-    auto fetch = [&](Tile& t, int key, int i) {
+    auto fetch = [&](Tile& t, int key, int i, unsigned at_code, unsigned at_scale) {
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             const int e = __builtin_amdgcn_readlane(half ? e1 : e0, i);
             t.e[half] = e;
-            const uint8_t* c = a.pool + ((size_t)(e >= 0 && e < a.d.n_blocks ? e : 0) * a.d.heads + h) * bytes;       // (no block: any one's memory, left out below)
+            const uint8_t* c = a.pool + ((size_t)(e >= 0 && e < a.d.n_blocks ? e : 0) * a.d.heads + it.h) * bytes;    // (no block: any one's memory, left out below)
             const int r = (key + 16 * half) & (a.d.block - 1);
             const uint8_t *kp = c + r * (HD / 2) + at_code, *vp = c + (a.d.block + r) * (HD / 2) + at_code;       // (scalar base, lane's offset)
             if constexpr (HD == 128) {
@@ -546,10 +557,37 @@ __global__ __launch_bounds__(256, (kv4_stream_waves<T, HD, RT>())) void kv4_stre
             t.vb[half] = (c + a.d.block * HD + (a.d.block + r) * (HD / 32))[at_scale];
         }
     };
-    if (k0 < end) fetch(now, k0, 0);
-    kv4_bf16x8 qf[RT][STEPS][NP];
-    Kv4Sight see[RT];
-    kv4_queries<T, HD, RT, NP>(a, s, h, p0, n16, g, [](int g_, int j) { return g_ * (HD / 4) + 8 * j; }, qf, see);
+    // opens the item at pos (which moves behind its units here); an item of which only its cost without keys lies here has units = 0
+    auto open = [&](int lane) {
+        const int n16 = lane & 15, g = lane >> 4;
+        int base;
+        it.seq = units.find(pos, base, it.s);
+        it.nb = Kv4Units::blocks(it.s.len);
+        const int cost = it.nb + KV4_ITEM_COST, at_item = kv4_div(pos - base, cost), from = pos - base - at_item * cost;
+        it.ti = a.tiles > 1 ? kv4_div(at_item, a.d.heads) : 0; it.h = at_item - it.ti * a.d.heads;
+        const int n = min(cost - from, stop - pos);
+        it.first = max(0, from - KV4_ITEM_COST); it.units = max(0, from + n - KV4_ITEM_COST) - it.first;
+        it.begins = pos - from + KV4_ITEM_COST;
+        pos += n;
+        const int p0 = it.ti * 16 * RT;
+        // keys of the item: no pair of it sees one from `limit` on, all see those below `all`
+        const int limit = a.mask ? it.s.len : it.s.len - it.s.rows + min(p0 + 16 * RT - 1, it.s.pairs - 1) / a.group + 1;
+        all = it.s.len - it.s.rows + (a.mask ? 0 : p0 / a.group + 1);
+        end = (int)min((long long)limit, (long long)(it.first + it.units) * KV4_UNIT);
+        row = a.table + (size_t)(a.row_start ? it.seq : a.seq0 + it.seq) * a.max_blocks;
+        k0 = it.first * KV4_UNIT + 32 * wave;
+        at = 0;
+        if (it.units == 0) { end = k0; return; }
+        entries(k0, lane);
+        kv4_queries<T, HD, RT>(a, it.s, it.h, p0, n16, g, [](int g_, int j) { return g_ * (HD / 4) + 8 * j; }, raw, see);
+        if (k0 < end) fetch(now, k0, 0, n16 * (HD / 2) + g * (HD / 8), n16 * (HD / 32) + g * (HD / 4) / 32);
+    };
+    open(threadIdx.x & 63);
+    int due[2] = {-1, -1}; Item due_it[2];       // items to report as arrived: one that began before, one that goes on
+    for (bool more = true; more;) {
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));                            // (what follows from it is not kept across items: 80 registers)
+    const int lane = tid & 63, n16 = lane & 15, g = lane >> 4;
     kv4_f32x4 o[RT][NB];
     float ref[RT], l[RT];
     unsigned no_number[RT];
@@ -559,10 +597,14 @@ __global__ __launch_bounds__(256, (kv4_stream_waves<T, HD, RT>())) void kv4_stre
 #pragma unroll
         for (int b = 0; b < NB; ++b) o[t][b] = kv4_f32x4{0.f, 0.f, 0.f, 0.f};
     }
+    if (it.units) {
+    kv4_bf16x8 qf[RT][STEPS][NP];
+    kv4_query_parts<T, HD, RT, NP>(a, raw, qf);
     for (; k0 < end; k0 += 32 * NW) {                        // (below 2^31: end is, and a step is short of the next block's last row)
         Tile t = now;
-        if (++at == 64) { entries(k0 + 32 * NW); at = 0; }
-        if (k0 + 32 * NW < end) fetch(now, k0 + 32 * NW, at);
+        if (++at == 64) { entries(k0 + 32 * NW, lane); at = 0; }
+        if (k0 + 32 * NW < end) fetch(now, k0 + 32 * NW, at, n16 * (HD / 2) + g * (HD / 8), n16 * (HD / 32) + g * (HD / 4) / 32);
+        // rows that are not held, and scales that say NaN, stay out of the products
         bool plain = k0 + 32 <= all;
         const bool there0 = t.e[0] >= 0 && t.e[0] < a.d.n_blocks, there1 = t.e[1] >= 0 && t.e[1] < a.d.n_blocks;
         const bool odd = t.kb[0] == 255 || t.vb[0] == 255 || t.kb[1] == 255 || t.vb[1] == 255;
@@ -570,7 +612,7 @@ __global__ __launch_bounds__(256, (kv4_stream_waves<T, HD, RT>())) void kv4_stre
         if (!plain || !there0 || !there1 || __any(odd)) {
             plain = false;
             held = (there0 ? 0xffffu : 0) | (there1 ? 0xffff0000u : 0);
-            if (k0 + 32 > s.len) held &= (1u << (s.len - k0)) - 1;               // (k0 < end <= len)
+            if (k0 + 32 > it.s.len) held &= (1u << (it.s.len - k0)) - 1;               // (k0 < end <= len)
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const bool in = held >> (16 * half + n16) & 1;
@@ -615,27 +657,26 @@ __global__ __launch_bounds__(256, (kv4_stream_waves<T, HD, RT>())) void kv4_stre
                 for (int r = 0; r < RT; ++r) o[r][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[r][0][p], o[r][b], 0, 0, 0);
         }
     }
-    // ---- the wavefronts' results, 16 pairs at a time.  Partials: two places per workgroup, one for an item that began before its run, one for an item that goes
-    // on behind it; a place: [pair][HD] sums, [pair] ref and denominator
+    }
+    const Item done = it;
+    more = pos < stop;
+    if (more) open(lane);                                    // (its requests travel while this one's results are put together)
+    if (done.units == 0) continue;
+    // ---- the wavefronts' results, 16 pairs at a time
     asm volatile("" : "+v"(tid));
-    const int n16_ = tid & 15, g_ = tid >> 4 & 3;
-    float* const mrg = (float*)lds;
-    const int count = min(16 * RT, pairs - p0);
-    const bool whole = n_units == nb;
-    constexpr int PLACE = 16 * RT * (HD + 2);
-    const Kv4Partials ws(a.ws, gridDim.x * (2u * PLACE * 4));
-    auto place = [&](int wg, bool begins_there) { return (2u * wg + begins_there) * PLACE; };
-    const unsigned part = place(blockIdx.x, first == 0);
+    const int n16_ = tid & 15, g_ = tid >> 4 & 3, p0 = done.ti * 16 * RT, count = min(16 * RT, done.s.pairs - p0);
+    const bool whole = done.units == done.nb, begins_here = done.first == 0;
+    const unsigned part = place(blockIdx.x, begins_here);
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         l[r] = kv4_xsum(l[r]);
         kv4_poison<NB>(no_number[r], o[r]);
-        __syncthreads();
+        kv4_lds_barrier();
         float* dst = mrg + (wave * 16 + n16_) * MSTRIDE;
 #pragma unroll
         for (int b = 0; b < NB; ++b) *(kv4_f32x4*)(dst + 16 * b + 4 * g_) = o[r][b];
         if (g_ == 0) *(float2*)(dst + HD) = make_float2(ref[r], l[r]);
-        __syncthreads();
+        kv4_lds_barrier();
         for (int i = tid; i < 16 * HD / 4; i += 256) {
             const int pr = i / (HD / 4), c = 4 * (i % (HD / 4));
             if (16 * r + pr >= count) break;
@@ -650,22 +691,32 @@ __global__ __launch_bounds__(256, (kv4_stream_waves<T, HD, RT>())) void kv4_stre
                 const float f = __builtin_amdgcn_exp2f(st.x - mx);
                 den += st.y * f; sum += *(const kv4_f32x4*)(src + c) * f;
             }
-            if (whole) kv4_store4<T, HD>(a, s, h, p0 + 16 * r + pr, c, sum * (den == 0.f ? 0.f : 1.f / den));         // (a row that sees nothing: zeros)
+            if (whole) kv4_store4<T, HD>(a, done.s, done.h, p0 + 16 * r + pr, c, sum * (den == 0.f ? 0.f : 1.f / den));    // (a row that sees nothing: zeros)
             else {
                 ws.put4(part + (16 * r + pr) * HD + c, sum);
                 if (c == 0) ws.put2(part + 16 * RT * HD + 2 * (16 * r + pr), mx, den);
             }
         }
     }
-    __syncthreads();                                         // (the next item's values go where these results were)
-    if (whole) continue;
-    // ---- arrival: the partials are acknowledged before the count that shows them
-    const int w0 = kv4_div(begins, per), parts = kv4_div(begins + nb - 1, per) - w0 + 1, item = (seq * a.tiles + ti) * a.d.heads + h;
+    kv4_lds_barrier();                                       // (the next item's values go where these results were)
+    if (!whole) { if (begins_here) { due_it[1] = done; due[1] = 0; } else { due_it[0] = done; due[0] = 0; } }
+    }
+    // ---- arrivals, all at the end of the run: the partials are acknowledged before the count that shows them
+    if (due[0] < 0 && due[1] < 0) return;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
+    for (int w = 0; w < 2; ++w) {
+    if (due[w] < 0) continue;
+    const int tid = threadIdx.x;
+    const Item x = due_it[w];
+    const Kv4Seq s = x.s;
+    const int h = x.h, p0 = x.ti * 16 * RT, count = min(16 * RT, s.pairs - p0);
+    const int w0 = kv4_div(x.begins, per), parts = kv4_div(x.begins + x.nb - 1, per) - w0 + 1, item = (x.seq * a.tiles + x.ti) * a.d.heads + h;
     if (tid == 0) last = __hip_atomic_fetch_add(&a.cnt[item], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == parts - 1;
     __syncthreads();
-    if (!last) continue;
+    const bool mine = last;
+    __syncthreads();
+    if (!mine) continue;
     if (tid == 0) __hip_atomic_store(&a.cnt[item], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     // Merge, in the order of the keys (the same whoever merges): a thread takes four dims of a pair and eight partials at a time, all requested at once with their
     // refs and denominators; where there are fewer pairs than threads for them, several threads share the partials and add up in LDS.
@@ -767,7 +818,11 @@ __global__ __launch_bounds__(256, 2) void kv4_rows_kernel(Kv4AttnArgs a) {
     fetch(0);
     kv4_bf16x8 qf[RT][STEPS][NP];
     Kv4Sight see[RT];
-    kv4_queries<T, HD, RT, NP>(a, s, h, min(w0, pairs - 1), n16, g, [](int g_, int j) { return 32 * j + 8 * g_; }, qf, see);
+    {
+        Kv4Raw<T> raw[RT][STEPS];
+        kv4_queries<T, HD, RT>(a, s, h, min(w0, pairs - 1), n16, g, [](int g_, int j) { return 32 * j + 8 * g_; }, raw, see);
+        kv4_query_parts<T, HD, RT, NP>(a, raw, qf);
+    }
     kv4_f32x4 o[RT][NB];
     float ref[RT], l[RT];
     unsigned no_number[RT];

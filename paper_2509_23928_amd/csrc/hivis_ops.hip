@@ -116,8 +116,8 @@ static Kv4Plan kv4_plan_attend(const Kv4Dims& d, bool f32, int group, int n_seqs
     p.rt = env_rt ? env_rt : pairs <= 16 ? 1 : pairs <= 32 || f32 ? 2 : 4;
     p.tiles = (int)((pairs + 16 * p.rt - 1) / (16 * p.rt));
     p.items = sh * p.tiles;
-    const long long most = env_wgs ? env_wgs : f32 ? 512 : 1024;
-    p.wgs = (int)std::min<long long>(most, p.items * std::max(1, (max_len + KV4_UNIT - 1) / KV4_UNIT));
+    const long long most = env_wgs ? env_wgs : 256 * (d.hd == 128 ? f32 ? 2 : 3 : f32 ? 3 : 4);
+    p.wgs = (int)std::min<long long>(most, p.items * (std::max(1, (max_len + KV4_UNIT - 1) / KV4_UNIT) + KV4_ITEM_COST));
     return p;
 }
 static long long kv4_counters(const Kv4Plan& p) { return (p.items * 4 + 255) / 256 * 256; }
@@ -237,7 +237,7 @@ int hivis_kv4_attend(void* hip_stream, const hivis_kv4_attention* a) {
     CHECK(a->n_rows >= 0 && (long long)a->n_rows * a->n_q_heads <= 0x7fffffffLL, "n_rows %d x n_q_heads %d", a->n_rows, a->n_q_heads);
     if (a->n_seqs == 0 || a->max_rows == 0 || a->n_rows == 0) return HIVIS_OK;
     CHECK(a->max_blocks >= 1 && (long long)a->max_blocks * k.d.block <= 0x7fffffffLL - 255, "max_blocks %d: a sequence's positions must be below 2^31 - 256", a->max_blocks);
-    CHECK((double)a->n_seqs * k.d.heads * (((long long)a->max_rows * (a->n_q_heads / k.d.heads) + 15) / 16) * ((long long)a->max_blocks * k.d.block / KV4_UNIT + 1) < 2147483648.0,
+    CHECK((double)a->n_seqs * k.d.heads * (((long long)a->max_rows * (a->n_q_heads / k.d.heads) + 15) / 16) * ((long long)a->max_blocks * k.d.block / KV4_UNIT + 1 + KV4_ITEM_COST) < 2147483648.0,
           "n_seqs %d, max_blocks %d, max_rows %d: more than a launch takes", a->n_seqs, a->max_blocks, a->max_rows);
     CHECK(!a->mask || a->max_rows <= 64, "max_rows %d: a mask has bits for 64 rows", a->max_rows);
     CHECK(std::isfinite(a->scale), "scale is not finite");
