@@ -271,9 +271,7 @@ struct Kv4AttnArgs {
 constexpr float KV4_REF0 = -1.0e30f;                         // ref before the first key (finite: a difference of two infinities would be no number)
 constexpr float KV4_SLACK = 8.f;
 constexpr int KV4_UNIT = 128;                                // keys of a unit of work: four wavefronts, 32 each
-#ifndef KV4_ITEM_COST
-constexpr int KV4_ITEM_COST = 2;
-#endif
+constexpr int KV4_ITEM_COST = 2;                             // what opening and closing an item costs, in units
 
 // LDS rows: the transposing read of four rows, and eight lanes' 16-byte accesses, meet all banks
 template <int HD> constexpr int kv4_vstride() { return HD * 2 + 32; }
@@ -455,7 +453,7 @@ struct Kv4Partials {
 };
 
 // ---- few rows: bound by the cache's bytes, or by latency ----
-// An item is 16 RT pairs of one key head of one sequence, a unit KV4_UNIT keys of an item; the units of all items in a row are dealt to the workgroups in equal runs, so
+// An item is 16 pairs of one key head of one sequence, a unit KV4_UNIT keys of an item; the units of all items in a row are dealt to the workgroups in equal runs, so
 // lengths as different as they come leave no workgroup idle (one workgroup per item and split of a fixed length: 54 us for 48 conversations of 30 to 16000 rows, and 41 with
 // the best length, where most of a grid sized for the longest had nothing to do).  An item that lies in several runs is merged by the workgroup that
 // finishes last.
@@ -503,10 +501,11 @@ struct Kv4Units {
     }
 };
 
-// wavefronts per SIMD that the kernel is compiled for
-template <typename T, int HD, int RT> constexpr int kv4_stream_waves() { return RT == 4 ? 1 : RT == 2 ? sizeof(T) == 4 && HD == 128 ? 1 : 2 : HD == 128 ? sizeof(T) == 4 ? 2 : 3 : sizeof(T) == 4 ? 3 : 4; }
-template <typename T, int HD, int RT>
-__global__ __launch_bounds__(256, (kv4_stream_waves<T, HD, RT>())) void kv4_stream_kernel(Kv4AttnArgs a) {
+// Workgroups per CU that the kernel is compiled for, with all registers that it wants (with one more per CU it spilled: 37 -> 47 us).  A launch has as many.
+template <typename T, int HD> constexpr int kv4_stream_per_cu() { return HD == 128 ? sizeof(T) == 4 ? 2 : 3 : sizeof(T) == 4 ? 3 : 4; }
+template <typename T, int HD>
+__global__ __launch_bounds__(256, (kv4_stream_per_cu<T, HD>())) void kv4_stream_kernel(Kv4AttnArgs a) {
+    constexpr int RT = 1;                                    // pairs of an item, in sixteens (32: 61 rows of 28 heads over 3075 rows 26 -> 49 us, and slower in 31 of 32 other shapes)
     constexpr int NP = sizeof(T) == 4 ? 3 : 1, STEPS = HD / 32, NB = HD / 16, VSTRIDE = kv4_vstride<HD>(), NW = 4;
     constexpr int MSTRIDE = HD + 4;                          // a pair's results in LDS: HD sums, ref, denominator
     constexpr int VB = NW * 32 * VSTRIDE, MB = NW * 16 * MSTRIDE * 4, PLACE = 16 * RT * (HD + 2);
@@ -780,9 +779,10 @@ __global__ __launch_bounds__(256, 2) void kv4_rows_kernel(Kv4AttnArgs a) {
     // before a tile's barrier, read behind it, cleared behind the next one.
     unsigned long long (*const odd)[3 + NG] = (unsigned long long (*)[3 + NG])(kv4_lds + 2 * BUF);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g = lane >> 4;
-    const int sh = blockIdx.x, ti = a.tiles - 1 - blockIdx.y;                    // (the longest first)
+    // (the longest first; sequences in turn, or each would always meet the same shader engine of a chiplet: four prompts of 641 to 3008 rows 405 us)
+    const int sh = blockIdx.x, ti = a.tiles - 1 - blockIdx.y;
     if (sh >= a.n_seqs * a.d.heads) return;
-    const int seq = sh / a.d.heads, h = sh - seq * a.d.heads;
+    const int h = sh % a.d.heads, seq = (int)((sh / a.d.heads + blockIdx.y) % a.n_seqs);
     const Kv4Seq s = kv4_seq(a, seq);
     const int pairs = s.pairs, p0 = ti * 64 * RT, w0 = p0 + wave * 16 * RT;
     if (p0 >= pairs) return;

@@ -8,7 +8,6 @@
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
-#include <cstdlib>
 #include <string>
 
 using namespace hivis;
@@ -101,27 +100,34 @@ int kv4_read_launch(hipStream_t st, int type, const RowsArgs& a) {
     return HIVIS_OK;
 }
 
-// How a call is cut: kernel, pairs per workgroup or item, row tiles of a sequence at most, workgroups.
+// How a call is cut: kernel, pairs per workgroup in sixty-fours (rows kernel), row tiles of a sequence at most, workgroups.
+// The kernel is the one with the shorter estimate, in us; all from calls of 1 to 256 key heads, 1 to 2000 rows, 500 to 6000 cached rows:
+//   stream: 8 us to open, merge and close (5.5 where no item is cut), and its 128-key units (16 pairs; two for each item) at the rate that a full chip reached;
+//   rows:   5.5 us, and the longer of its 64-key tiles one after the other (few workgroups: their latency) and all steps of 64 pairs x 64 keys at the full rate.
+// 61 rows of 28 heads over 3000 rows: stream 26 us, rows 112; 128 rows of 32 heads over 628: 17 and 21; 256 rows of 32 heads over themselves: 14 and 11;
+// 1024 rows of 32 heads: 57 and 32.  Two tiles of pairs per wavefront only in bf16 and only where the chip is full: 2000 rows x 4 of 32 heads 264 -> 182 us, but
+// 640 rows of 32 heads 21 -> 23 (fp32 spills: 377 -> 335 and 64 rows over 3000 rows 119 -> 176).
 struct Kv4Plan { bool rows; int rt, tiles, wgs; long long items; };
 static Kv4Plan kv4_plan_attend(const Kv4Dims& d, bool f32, int group, int n_seqs, int max_rows, int max_len) {
-    static const int env_rows = getenv("KV4_ROWS") ? atoi(getenv("KV4_ROWS")) : 0, env_rt = getenv("KV4_RT") ? atoi(getenv("KV4_RT")) : 0, env_wgs = getenv("KV4_WGS") ? atoi(getenv("KV4_WGS")) : 0;
     const long long pairs = (long long)max_rows * group, sh = (long long)n_seqs * d.heads;
+    const int form = (d.hd == 128 ? 0 : 1) + (f32 ? 2 : 0);
+    static const double unit_rate[4] = {350, 600, 260, 400}, tile_us[2][4] = {{1.45, 1.0, 2.3, 1.55}, {1.65, 1.35, 0, 0}}, step_rate[2][4] = {{248, 525, 173, 319}, {350, 605, 0, 0}};
+    const double keys = std::max(1.0, max_len - 0.5 * max_rows);         // that a row sees on average
     Kv4Plan p{};
-    p.rows = env_rows ? pairs >= env_rows : pairs >= 256;
-    if (p.rows) {
-        p.rt = env_rt ? env_rt : !f32 && sh * ((pairs + 127) / 128) >= 512 ? 2 : 1;
-        p.tiles = (int)((pairs + 64 * p.rt - 1) / (64 * p.rt));
-        return p;
-    }
-    p.rt = env_rt ? env_rt : pairs <= 16 ? 1 : pairs <= 32 || f32 ? 2 : 4;
-    p.tiles = (int)((pairs + 16 * p.rt - 1) / (16 * p.rt));
+    p.tiles = (int)((pairs + 15) / 16);
     p.items = sh * p.tiles;
-    const long long most = env_wgs ? env_wgs : 256 * (d.hd == 128 ? f32 ? 2 : 3 : f32 ? 3 : 4);
-    p.wgs = (int)std::min<long long>(most, p.items * (std::max(1, (max_len + KV4_UNIT - 1) / KV4_UNIT) + KV4_ITEM_COST));
+    p.wgs = (int)std::min<double>(256 * (f32 ? d.hd == 128 ? kv4_stream_per_cu<float, 128>() : kv4_stream_per_cu<float, 64>() : d.hd == 128 ? kv4_stream_per_cu<__bf16, 128>() : kv4_stream_per_cu<__bf16, 64>()),
+                                  (double)p.items * (std::max(1, (int)(((long long)max_len + KV4_UNIT - 1) / KV4_UNIT)) + KV4_ITEM_COST));
+    double best = (max_len > KV4_UNIT ? 8.0 : 5.5) + p.items * (keys / KV4_UNIT + 0.5 + KV4_ITEM_COST) / unit_rate[form];
+    for (int rt = 1; rt <= (f32 ? 1 : 2); ++rt) {
+        const long long tiles = (pairs + 64 * rt - 1) / (64 * rt);
+        const double us = 5.5 + std::max((max_len + 63) / 64 * tile_us[rt - 1][form], sh * tiles * rt * (keys / 64 + 0.5) / step_rate[rt - 1][form]);
+        if (us < best) { best = us; p.rows = true; p.rt = rt; p.tiles = (int)tiles; }
+    }
     return p;
 }
 static long long kv4_counters(const Kv4Plan& p) { return (p.items * 4 + 255) / 256 * 256; }
-static long long kv4_space(const Kv4Plan& p, int hd) { return p.rows ? 16 : kv4_counters(p) + 2LL * p.wgs * 16 * p.rt * (hd + 2) * 4; }
+static long long kv4_space(const Kv4Plan& p, int hd) { return p.rows ? 16 : kv4_counters(p) + 2LL * p.wgs * 16 * (hd + 2) * 4; }
 
 int kv4_attend_launch(hipStream_t st, int dtype, Kv4AttnArgs a, int max_rows, int max_len, void* ws) {
     const bool f32 = dtype == HIVIS_F32;
@@ -134,16 +140,13 @@ int kv4_attend_launch(hipStream_t st, int dtype, Kv4AttnArgs a, int max_rows, in
         OP_TRY(hipFuncSetAttribute((const void*)kv4_rows_kernel<T_, HD_, RT_>, hipFuncAttributeMaxDynamicSharedMemorySize, lds_));                            \
         hipLaunchKernelGGL((kv4_rows_kernel<T_, HD_, RT_>), dim3((unsigned)sh, p.tiles), dim3(256), lds_, st, a);                                             \
     } while (0)
-#define KV4_STREAM_(T_, HD_, RT_) hipLaunchKernelGGL((kv4_stream_kernel<T_, HD_, RT_>), dim3(p.wgs), dim3(256), 0, st, a)
 #define KV4_FORMS(T_, HD_)                                                                                      \
-    if (p.rows) { if (p.rt == 1) KV4_ROWS_(T_, HD_, 1); else KV4_ROWS_(T_, HD_, 2); }                           \
-    else if (p.rt == 1) KV4_STREAM_(T_, HD_, 1);                                                                 \
-    else if (p.rt == 2) KV4_STREAM_(T_, HD_, 2);                                                                 \
-    else KV4_STREAM_(T_, HD_, 4);
+    if (!p.rows) hipLaunchKernelGGL((kv4_stream_kernel<T_, HD_>), dim3(p.wgs), dim3(256), 0, st, a);            \
+    else if (p.rt == 1) KV4_ROWS_(T_, HD_, 1);                                                                  \
+    else if constexpr (sizeof(T_) == 2) KV4_ROWS_(T_, HD_, 2);
     if (f32) { if (a.d.hd == 128) { KV4_FORMS(float, 128) } else { KV4_FORMS(float, 64) } }
     else { if (a.d.hd == 128) { KV4_FORMS(__bf16, 128) } else { KV4_FORMS(__bf16, 64) } }
 #undef KV4_FORMS
-#undef KV4_STREAM_
 #undef KV4_ROWS_
     OP_TRY(hipGetLastError());
     return HIVIS_OK;
