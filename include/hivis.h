@@ -329,7 +329,7 @@ int hivis_kv4_attend(void *hip_stream, const hivis_kv4_attention *a);
 
 /* Log probabilities of given tokens under softmax(logits / temperature), the entropy of each row (in nats), and its top_k
  * most probable tokens (the larger logit first, then the lower id).
- *   logits: HIVIS_F32 or HIVIS_BF16, [n_rows][vocab], rows row_stride values apart.   tokens [n_rows][n_tokens].
+ *   logits: HIVIS_F32 or HIVIS_BF16, [n_rows][vocab], rows row_stride values apart; n_rows <= 65535.   tokens [n_rows][n_tokens].
  *   logprob [n_rows][n_tokens]; entropy [n_rows] (may be NULL); top_ids, top_logprobs [n_rows][top_k], top_k <= 32.
  * A token outside [0, vocab) gives NaN.  A row with a NaN or without a finite maximum gives NaN everywhere and ids -1.
  * Errors: EINVAL, EHIP. */

@@ -16,7 +16,7 @@ int kv4_append_launch(hipStream_t st, int type, const RowsArgs& a);
 int kv4_read_launch(hipStream_t st, int type, const RowsArgs& a);
 int kv4_attend_launch(hipStream_t st, int dtype, Kv4AttnArgs a, int max_rows, int max_len, void* ws);
 long long kv4_attend_space(const Kv4Dims& d, int dtype, int n_q_heads, int n_seqs, int max_rows, int max_len);
-int logprobs_launch(hipStream_t st, int dtype, const LogprobsArgs& a, void* ws, long long ws_bytes);
+int logprobs_launch(hipStream_t st, int dtype, LogprobsArgs a, void* ws);
 long long logprobs_space(int rows, int vocab, int top);
 
 }  // namespace hivis

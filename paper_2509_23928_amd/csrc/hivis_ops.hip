@@ -156,16 +156,31 @@ long long kv4_attend_space(const Kv4Dims& d, int dtype, int n_q_heads, int n_seq
     return kv4_space(kv4_plan_attend(d, dtype == HIVIS_F32, n_q_heads / d.heads, n_seqs, max_rows, max_len), d.hd);
 }
 
-int logprobs_launch(hipStream_t st, int dtype, const LogprobsArgs& a, void* ws, long long ws_bytes) {
-    (void)ws; (void)ws_bytes;
+// Segments of a row: enough workgroups for four to a CU, of at least one chunk
+static void logprobs_cut(int rows, int vocab, int* chunks, int* segs) {
+    const int all = (vocab - 1) / LOGPROBS_CHUNK + 1, want = std::max(1, std::min(all, LOGPROBS_WGS / std::max(rows, 1)));
+    *chunks = (all + want - 1) / want;
+    *segs = (all + *chunks - 1) / *chunks;
+}
+static long long logprobs_counters(int rows) { return ((long long)rows * 4 + 255) / 256 * 256; }
+
+int logprobs_launch(hipStream_t st, int dtype, LogprobsArgs a, void* ws) {
     if (a.rows == 0) return HIVIS_OK;
-    if (dtype == HIVIS_F32) hipLaunchKernelGGL(logprobs_kernel<float>, dim3(a.rows), dim3(1024), 0, st, a);
-    else hipLaunchKernelGGL(logprobs_kernel<__bf16>, dim3(a.rows), dim3(1024), 0, st, a);
+    logprobs_cut(a.rows, a.vocab, &a.chunks, &a.segs);
+    a.cnt = (int*)ws; a.part = (uint32_t*)((char*)ws + logprobs_counters(a.rows));
+#define LOGPROBS_(T_, TOP_) hipLaunchKernelGGL((logprobs_kernel<T_, TOP_>), dim3(a.segs, a.rows), dim3(LOGPROBS_NT), 0, st, a)
+    if (dtype == HIVIS_F32) { if (a.top) LOGPROBS_(float, true); else LOGPROBS_(float, false); }
+    else { if (a.top) LOGPROBS_(__bf16, true); else LOGPROBS_(__bf16, false); }
+#undef LOGPROBS_
     OP_TRY(hipGetLastError());
     return HIVIS_OK;
 }
 
-long long logprobs_space(int rows, int vocab, int top) { (void)rows; (void)vocab; (void)top; return 16; }
+long long logprobs_space(int rows, int vocab, int top) {
+    int chunks, segs;
+    logprobs_cut(rows, vocab, &chunks, &segs);
+    return logprobs_counters(rows) + (segs > 1 ? (long long)rows * segs * (LOGPROBS_STATS + 2 * top) * 4 : 0) + 16;
+}
 
 }  // namespace hivis
 
@@ -261,7 +276,8 @@ int hivis_kv4_attend(void* hip_stream, const hivis_kv4_attention* a) {
 }
 
 static int check_logprobs(int32_t n_rows, int32_t vocab, int32_t top_k) {
-    CHECK(n_rows >= 0 && vocab >= 1, "n_rows %d, vocab %d", n_rows, vocab);
+    CHECK(n_rows >= 0 && n_rows <= 65535, "n_rows %d outside [0,65535]", n_rows);
+    CHECK(vocab >= 1 && vocab <= 0x7fffffff - LOGPROBS_CHUNK, "vocab %d", vocab);
     CHECK(top_k >= 0 && top_k <= LOGPROBS_MAX_TOP && top_k <= vocab, "top_k %d outside [0,%d] or above vocab %d", top_k, LOGPROBS_MAX_TOP, vocab);
     return HIVIS_OK;
 }
@@ -287,7 +303,7 @@ int hivis_logprobs(void* hip_stream, int32_t dtype, const void* logits, int64_t 
     if (int rc = check_devices({{logits, "logits"}, {n_tokens ? tokens : nullptr, "tokens"}, {n_tokens ? logprob : nullptr, "logprob"}, {entropy, "entropy"}, {top_k ? top_ids : nullptr, "top_ids"},
                                 {top_k ? top_logprobs : nullptr, "top_logprobs"}, {workspace, "workspace"}})) return rc;
     return logprobs_launch((hipStream_t)hip_stream, dtype,
-                           LogprobsArgs{logits, row_stride, n_rows, vocab, inv, tokens, n_tokens, logprob, entropy, top_k, top_ids, top_logprobs}, workspace, workspace_bytes);
+                           LogprobsArgs{logits, row_stride, n_rows, vocab, inv, tokens, n_tokens, logprob, entropy, top_k, top_ids, top_logprobs, 0, 0, nullptr, nullptr}, workspace);
 }
 
 }  // extern "C"
