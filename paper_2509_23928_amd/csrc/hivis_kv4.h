@@ -33,70 +33,104 @@ __host__ __device__ inline int kv4_scale_byte(unsigned a) {
 }
 
 // ---- plan ------------------------------------------------------------------------------------------------------------------------------
-// One workgroup; sequences in rounds of its 1024 threads.  Three sums over the sequences in order (rows, blocks given back from the last sequence on,
-// blocks taken) decide everything, so the result does not depend on timing.  Latency bound: the sums, then one pass over the slots.
-constexpr int PLAN_NT = 1024;
+// Three sums over the sequences in order (rows, blocks given back from the last sequence on, blocks taken) decide everything, so the result does not depend on
+// timing.  Latency bound: one workgroup, a wavefront for every 64 sequences up to sixteen (and rounds of 1024 beyond), sums in registers, one batch of requests
+// per step; blocks are moved by all threads, a block each.  The slots of many rows are a launch of their own, over the chip (plan_fused).
+constexpr int PLAN_MAX = 1024;                               // threads at most
 
 struct PlanArgs {
     int n, max_blocks, shift, n_blocks, max_rows;
     const int *keep, *add; int *held, *table, *free_list, *row_start, *slots, *positions, *status;
+    bool fill;                                               // slots and positions in the same launch
 };
+
+struct PlanShared { long long part[PLAN_MAX / 64]; int from[PLAN_MAX], base[PLAN_MAX], s[PLAN_MAX]; };
 
 // inclusive sum over the workgroup's threads (64-bit: adds of many sequences pass 32 bits)
 __device__ inline long long plan_scan(long long x, long long* part, long long* total) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) { const long long y = __shfl_up(x, d); if (lane >= d) x += y; }
+    if (waves == 1) { *total = __shfl(x, 63); return x; }
     if (lane == 63) part[wave] = x;
     __syncthreads();
     long long before = 0, all = 0;
-    for (int w = 0; w < PLAN_NT / 64; ++w) { if (w < wave) before += part[w]; all += part[w]; }
+    for (int w = 0; w < waves; ++w) { if (w < wave) before += part[w]; all += part[w]; }
     __syncthreads();
     *total = all;
     return x + before;
 }
 
-// what sequence s asks for: status 2 if it cannot be meant (lengths below zero, more rows kept than its blocks hold, longer than its table row)
-__device__ inline int plan_need(const PlanArgs& a, int s, int& keep, int& add, int& held) {
-    keep = a.keep[s]; add = a.add[s]; held = a.held[s];
+// what sequence s asks for, in blocks; -1 if it cannot be meant (lengths below zero, more rows kept than its blocks hold, longer than its table row)
+__device__ inline int plan_need(const PlanArgs& a, int keep, int add, int held) {
     const long long end = (long long)keep + add, room = (long long)held << a.shift;
     if (keep < 0 || add < 0 || held < 0 || held > a.max_blocks || keep > room || end > ((long long)a.max_blocks << a.shift)) return -1;
     return (int)((end + (1 << a.shift) - 1) >> a.shift);
 }
 
-__global__ __launch_bounds__(PLAN_NT) void kv4_plan_kernel(PlanArgs a) {
-    __shared__ long long part[PLAN_NT / 64];
-    const int t = threadIdx.x;
+// Blocks of the round's sequences, a thread each: `n` of this thread's sequence s (upto: with those of the threads before it, all in total), from its block `from` on.
+// f(sequence, block index, position among the round's blocks)
+template <typename F>
+__device__ inline void plan_blocks(PlanShared& sh, int s, int n, int from, long long upto, long long total, F f) {
+    sh.s[threadIdx.x] = s; sh.from[threadIdx.x] = from; sh.base[threadIdx.x] = (int)upto;
+    __syncthreads();
+    for (long long i = threadIdx.x; i < total; i += blockDim.x) {
+        int lo = 0, hi = blockDim.x - 1;                     // the first thread whose blocks end behind i
+        while (lo < hi) { const int mid = (lo + hi) >> 1; if (sh.base[mid] > i) hi = mid; else lo = mid + 1; }
+        const int before = lo ? sh.base[lo - 1] : 0;
+        f(sh.s[lo], sh.from[lo] + (int)i - before, (int)i);
+    }
+    __syncthreads();
+}
+
+__device__ inline void plan_fill(const PlanArgs& a, int r, int total) {
+    int slot = -1, pos = -1;
+    if (r < total) {
+        int lo = 0, hi = a.n - 1;                            // the last sequence that starts at or before r
+        while (lo < hi) { const int mid = (lo + hi + 1) >> 1; if (a.row_start[mid] <= r) lo = mid; else hi = mid - 1; }
+        pos = a.keep[lo] + r - a.row_start[lo];
+        slot = (a.table[(size_t)lo * a.max_blocks + (pos >> a.shift)] << a.shift) + (pos & ((1 << a.shift) - 1));
+    }
+    a.slots[r] = slot;
+    if (a.positions) a.positions[r] = pos;
+}
+
+__global__ __launch_bounds__(PLAN_MAX) void kv4_plan_kernel(PlanArgs a) {
+    __shared__ PlanShared sh;
+    const int t = threadIdx.x, threads = blockDim.x, rounds = (a.n + threads - 1) / threads;
     // a list whose count is no count of blocks gives nothing
     int count = a.free_list[0];
     if (count < 0 || count > a.n_blocks) count = 0;
-    __syncthreads();
-    // ---- rows in order: who has room among the slots; blocks given back
+    // One round: everything stays in registers.  More: what a sequence asks for is read again for every sum (held changes only where blocks are given back).
+    int keep = 0, add = 0, held = 0, need = -1, status = 0;
+    auto load = [&](int s) { keep = add = held = 0; need = -1; if (s < a.n) { keep = a.keep[s]; add = a.add[s]; held = a.held[s]; need = plan_need(a, keep, add, held); } };
     long long rows = 0, total;
-    for (int s0 = 0; s0 < a.n; s0 += PLAN_NT) {
-        const int s = s0 + t;
-        int keep = 0, add = 0, held = 0, need = -1;
-        if (s < a.n) need = plan_need(a, s, keep, add, held);
-        const long long upto = rows + plan_scan(need >= 0 ? add : 0, part, &total);
+    // ---- rows in order: who has room among the slots
+    for (int r = 0; r < rounds; ++r) {
+        const int s = r * threads + t;
+        load(s);
+        const long long upto = rows + plan_scan(need >= 0 ? add : 0, sh.part, &total);
         rows += total;
-        if (s < a.n) a.status[s] = need < 0 ? 2 : upto > a.max_rows ? 3 : 0;
+        status = need < 0 ? 2 : upto > a.max_rows ? 3 : 0;
+        if (s < a.n && rounds > 1) a.status[s] = status;
     }
+    // ---- blocks given back, the last sequence's last block first
     __syncthreads();
-    for (int s0 = (a.n - 1) / PLAN_NT * PLAN_NT; s0 >= 0; s0 -= PLAN_NT) {       // the last sequence first
-        const int s = s0 + PLAN_NT - 1 - t;
-        int keep, add, held = 0, need = 0;
-        bool give = false;
-        if (s < a.n && a.status[s] == 0) { need = plan_need(a, s, keep, add, held); give = need < held; }
-        const int n = give ? held - need : 0;
-        int at = count + (int)(plan_scan(n, part, &total) - n);
-        count = (int)min((long long)a.n_blocks, count + total);
-        if (give) {
-            int* row = a.table + (size_t)s * a.max_blocks;
-            for (int j = held - 1; j >= need; --j, ++at) {
-                if (at < a.n_blocks) a.free_list[1 + at] = row[j];               // (more blocks than there are: the tables were not this pool's)
-                row[j] = -1;
-            }
-            a.held[s] = need;
+    for (int r = rounds - 1; r >= 0; --r) {
+        const int s = r * threads + t;
+        if (rounds > 1) { load(s); status = s < a.n ? a.status[s] : 2; }
+        const int n = status == 0 && need >= 0 ? max(held - need, 0) : 0;
+        const long long upto = plan_scan(n, sh.part, &total);
+        if (total) {
+            const long long all = total;
+            plan_blocks(sh, s, n, need, upto, total, [&](int seq, int j, int i) {
+                const long long at = count + (all - 1 - i);              // (more blocks than there are: the tables were not this pool's)
+                int* b = a.table + (size_t)seq * a.max_blocks + j;
+                if (at < a.n_blocks) a.free_list[1 + at] = *b;
+                *b = -1;
+            });
+            if (n) { held = need; a.held[s] = need; }
+            count = (int)min((long long)a.n_blocks, count + total);
         }
     }
     __threadfence_block();
@@ -104,44 +138,38 @@ __global__ __launch_bounds__(PLAN_NT) void kv4_plan_kernel(PlanArgs a) {
     // ---- blocks taken from the top of the list, in order of the sequences; row starts
     long long want = 0, start = 0;
     int left = count;
-    for (int s0 = 0; s0 < a.n; s0 += PLAN_NT) {
-        const int s = s0 + t;
-        int keep = 0, add = 0, held = 0, need = 0, n = 0;
-        bool ok = s < a.n && a.status[s] == 0;
-        if (ok) { need = plan_need(a, s, keep, add, held); n = max(need - held, 0); }
-        const long long upto = want + plan_scan(n, part, &total);
-        want += total;
-        if (ok && n > 0) {
-            if (upto > count) { ok = false; a.status[s] = 1; }
-            else {
-                int* row = a.table + (size_t)s * a.max_blocks;
-                const int top = count - (int)(upto - n);                         // list entry 1 + (top - 1) is the next one
-                for (int j = 0; j < n; ++j) row[held + j] = a.free_list[top - j];
-                a.held[s] = need;
-            }
+    for (int r = 0; r < rounds; ++r) {
+        const int s = r * threads + t;
+        if (rounds > 1) { load(s); status = s < a.n ? a.status[s] : 2; }
+        const int n = status == 0 && need >= 0 ? max(need - held, 0) : 0;
+        const long long upto = want + plan_scan(n, sh.part, &total);
+        if (n > 0 && upto > count) status = 1;
+        // those before the first that is refused are served, so what is taken is a run from the top
+        const int mine = status == 0 ? n : 0;
+        long long taken = total;
+        if (want + total > count) (void)plan_scan(mine, sh.part, &taken);
+        if (taken) {
+            const int top = count - (int)want;               // list entry `top` is the next one
+            plan_blocks(sh, s, mine, held, taken == total ? upto - want : min(upto - want, taken), taken, [&](int seq, int j, int i) { a.table[(size_t)seq * a.max_blocks + j] = a.free_list[top - i]; });
+            if (mine) a.held[s] = need;
         }
-        (void)plan_scan(ok ? n : 0, part, &total);
-        left -= (int)total;
-        const int mine = ok ? add : 0;
-        const long long end = start + plan_scan(mine, part, &total);
+        want += total;
+        left -= (int)taken;
+        const int lines = status == 0 && s < a.n ? add : 0;
+        const long long end = start + plan_scan(lines, sh.part, &total);
         start += total;
-        if (s < a.n) a.row_start[s] = (int)(end - mine);
+        if (s < a.n) { a.row_start[s] = (int)(end - lines); a.status[s] = status; }
     }
     if (t == 0) { a.row_start[a.n] = (int)start; a.free_list[0] = left; }
+    if (!a.fill) return;
     __threadfence_block();
     __syncthreads();
-    // ---- slots and positions of the rows; -1 behind the last
-    for (int r = t; r < a.max_rows; r += PLAN_NT) {
-        int slot = -1, pos = -1;
-        if (r < (int)start) {
-            int lo = 0, hi = a.n - 1;                                            // the last sequence that starts at or before r
-            while (lo < hi) { const int mid = (lo + hi + 1) >> 1; if (a.row_start[mid] <= r) lo = mid; else hi = mid - 1; }
-            pos = a.keep[lo] + r - a.row_start[lo];
-            slot = (a.table[(size_t)lo * a.max_blocks + (pos >> a.shift)] << a.shift) + (pos & ((1 << a.shift) - 1));
-        }
-        a.slots[r] = slot;
-        if (a.positions) a.positions[r] = pos;
-    }
+    for (int r = t; r < a.max_rows; r += threads) plan_fill(a, r, (int)start);
+}
+
+__global__ __launch_bounds__(256) void kv4_plan_slots_kernel(PlanArgs a) {
+    const int r = blockIdx.x * 256 + threadIdx.x;
+    if (r < a.max_rows) plan_fill(a, r, a.row_start[a.n]);
 }
 
 // ---- append and read ----------------------------------------------------------------------------------------------------------------------

@@ -11,7 +11,7 @@ enum { KV4_ROWS_F32 = 0, KV4_ROWS_BF16 = 1, KV4_ROWS_HALVES = 2 };
 void set_thread_error(const char* message);                  // what hivis_last_error(NULL) returns on this thread
 int op_fail(int code, const char* fmt, ...);
 
-int kv4_plan_launch(hipStream_t st, const PlanArgs& a);
+int kv4_plan_launch(hipStream_t st, PlanArgs a);
 int kv4_append_launch(hipStream_t st, int type, const RowsArgs& a);
 int kv4_read_launch(hipStream_t st, int type, const RowsArgs& a);
 int kv4_attend_launch(hipStream_t st, int dtype, Kv4AttnArgs a, int max_rows, int max_len, void* ws);
