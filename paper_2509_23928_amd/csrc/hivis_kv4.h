@@ -194,53 +194,75 @@ template <> __device__ inline void kv4_load8<__bf16>(const __bf16* p, float (&x)
     for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(u[i] << 16); x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
 }
 
-// place of one group of eight dims: its code word and (for the group's first eight) scale byte
+// Grid of append and read: lanes over a row's keys, then its values, eight dims each (x), and RPT rows per thread (y, in rounds of the grid): no quotients, the slots in
+// scalar registers, RPT requests under way.
+struct Kv4Lane { int kv, h, piece; long long at; bool in; };         // at: of its eight dims in a row (values)
+__device__ inline Kv4Lane kv4_lane(const RowsArgs& a) {
+    const int i = blockIdx.x * 256 + threadIdx.x, sh = a.d.hd == 128 ? 4 : 3, half = a.d.heads << sh;
+    Kv4Lane l;
+    l.in = i < 2 * half;
+    l.kv = i >= half;
+    l.h = (i - l.kv * half) >> sh; l.piece = i & ((1 << sh) - 1);
+    l.at = (long long)l.h * a.head + l.piece * 8;
+    return l;
+}
+// places of those dims in a slot's block: code word, and scale byte of the group that they belong to
 struct Kv4Place { uint8_t *code, *scale; };
-__device__ inline Kv4Place kv4_place(const Kv4Dims& d, uint8_t* pool, int slot, int h, int kv, int piece) {
+__device__ inline Kv4Place kv4_place(const Kv4Dims& d, uint8_t* pool, int slot, const Kv4Lane& l) {
     const int r = slot & (d.block - 1);
-    uint8_t* c = pool + ((size_t)(slot >> d.shift) * d.heads + h) * kv4_chunk(d.hd, d.block);
-    return {c + (size_t)kv * d.block * (d.hd / 2) + r * (d.hd / 2) + piece * 4, c + (size_t)d.block * d.hd + (size_t)kv * d.block * (d.hd / 32) + r * (d.hd / 32) + piece / 4};
+    uint8_t* c = pool + ((size_t)(slot >> d.shift) * d.heads + l.h) * kv4_chunk(d.hd, d.block);
+    return {c + (l.kv * d.block + r) * (d.hd / 2) + l.piece * 4, c + d.block * d.hd + (l.kv * d.block + r) * (d.hd / 32) + l.piece / 4};
+}
+__device__ inline int kv4_slot(const RowsArgs& a, int r) {           // -1: the row is left out
+    const int slot = r < a.n ? a.slots[r] : -1;
+    return slot >= 0 && (slot >> a.d.shift) < a.d.n_blocks ? slot : -1;
 }
 
 // A lane per eight dims: 16 or 32 bytes in, one word of codes out; four lanes agree on the group's scale.  Bound by the rows it reads.
 // (Magnitudes are compared as integers: a NaN is then the largest, which fmax would drop.)
-template <typename T>
+template <typename T, int RPT>
 __global__ __launch_bounds__(256) void kv4_append_kernel(RowsArgs a) {
-    const int pieces = a.d.hd / 8;
-    const long long i = (long long)blockIdx.x * 256 + threadIdx.x, all = (long long)a.n * a.d.heads * 2 * pieces;
-    if (i >= all) return;                                   // (whole groups of four lanes: all is a multiple of 8)
-    const int piece = (int)(i % pieces), kv = (int)(i / pieces) & 1;
-    const long long rh = i / (2 * pieces);
-    const int h = (int)(rh % a.d.heads), r = (int)(rh / a.d.heads);
-    const int slot = a.slots[r];
-    if (slot < 0 || (slot >> a.d.shift) >= a.d.n_blocks) return;
-    long long at = (long long)r * a.row;
-    if (a.first) at = (long long)(r / a.m) * a.seq + ((long long)a.first[r / a.m] + a.offset + r % a.m) * a.row;
-    at += (long long)h * a.head;
-    float x[8];
-    if constexpr (sizeof(T) == 1) {
-        const _Float16* p = (const _Float16*)(kv ? a.v : a.k) + 2 * at + piece * 8;
-        typedef _Float16 h8 __attribute__((ext_vector_type(8)));
-        const h8 hi = *(const h8*)p, lo = *(const h8*)(p + a.d.hd);
+    const Kv4Lane l = kv4_lane(a);
+    if (!l.in) return;                                       // (whole groups of four lanes)
+    const char* const base = (const char*)(l.kv ? a.v : a.k);
+    for (int r0 = blockIdx.y * RPT; r0 < a.n; r0 += gridDim.y * RPT) {
+        float x[RPT][8];
+        int slot[RPT];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = (float)hi[e] + (float)lo[e];
-    } else kv4_load8<T>((const T*)(kv ? a.v : a.k) + at + piece * 8, x);
-    unsigned m = 0;
+        for (int u = 0; u < RPT; ++u) slot[u] = kv4_slot(a, r0 + u);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(x[e]) & 0x7fffffffu);
-    m = max(m, (unsigned)__shfl_xor((int)m, 1)); m = max(m, (unsigned)__shfl_xor((int)m, 2));
-    const int b = kv4_scale_byte(m);
-    const float scale = __uint_as_float((unsigned)(b == 255 ? 127 : b) << 23);
-    unsigned code = 0;
-    if (b != 255) {
-        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[0], x[1], scale, 0);
-        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[2], x[3], scale, 1);
-        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[4], x[5], scale, 2);
-        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[6], x[7], scale, 3);
+        for (int u = 0; u < RPT; ++u) {
+            const int r = min(r0 + u, a.n - 1);              // (a row that is left out is read, not written)
+            long long at = (long long)r * a.row;
+            if (a.first) at = (long long)(r / a.m) * a.seq + ((long long)a.first[r / a.m] + a.offset + r % a.m) * a.row;
+            at += l.at;
+            if constexpr (sizeof(T) == 1) {
+                typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+                const _Float16* p = (const _Float16*)base + 2 * (at - l.piece * 8) + l.piece * 8;
+                const h8 hi = *(const h8*)p, lo = *(const h8*)(p + a.d.hd);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[u][e] = (float)hi[e] + (float)lo[e];
+            } else kv4_load8<T>((const T*)base + at, x[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < RPT; ++u) {
+            unsigned m = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(x[u][e]) & 0x7fffffffu);
+            m = max(m, (unsigned)__builtin_amdgcn_update_dpp(0, (int)m, 0xB1, 0xf, 0xf, false)); m = max(m, (unsigned)__builtin_amdgcn_update_dpp(0, (int)m, 0x4E, 0xf, 0xf, false));
+            const int b = kv4_scale_byte(m);
+            const float scale = __uint_as_float((unsigned)(b == 255 ? 127 : b) << 23);
+            unsigned code = 0;
+            code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[u][0], x[u][1], scale, 0);
+            code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[u][2], x[u][3], scale, 1);
+            code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[u][4], x[u][5], scale, 2);
+            code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[u][6], x[u][7], scale, 3);
+            if (slot[u] < 0) continue;
+            const Kv4Place p = kv4_place(a.d, a.pool, slot[u], l);
+            *(unsigned*)p.code = b == 255 ? 0 : code;
+            if ((l.piece & 3) == 0) *p.scale = (uint8_t)b;
+        }
     }
-    const Kv4Place p = kv4_place(a.d, a.pool, slot, h, kv, piece);
-    *(unsigned*)p.code = code;
-    if ((piece & 3) == 0) *p.scale = (uint8_t)b;
 }
 
 // the value of code c (four bits) at a scale
@@ -250,29 +272,36 @@ __device__ inline float kv4_value(unsigned c, float scale) {
     return ((c & 8) ? -x : x) * scale;
 }
 
-template <typename T>
+template <typename T, int RPT>
 __global__ __launch_bounds__(256) void kv4_read_kernel(RowsArgs a) {
-    const int pieces = a.d.hd / 8;
-    const long long i = (long long)blockIdx.x * 256 + threadIdx.x, all = (long long)a.n * a.d.heads * 2 * pieces;
-    if (i >= all) return;
-    const int piece = (int)(i % pieces), kv = (int)(i / pieces) & 1;
-    const long long rh = i / (2 * pieces);
-    const int h = (int)(rh % a.d.heads), r = (int)(rh / a.d.heads);
-    const int slot = a.slots[r];
-    if (slot < 0 || (slot >> a.d.shift) >= a.d.n_blocks) return;
-    const Kv4Place p = kv4_place(a.d, a.pool, slot, h, kv, piece);
-    const unsigned code = *(const unsigned*)p.code, b = *p.scale;
-    const float scale = b == 255 ? __uint_as_float(0x7fc00000u) : __uint_as_float(b << 23);
-    float x[8];
+    const Kv4Lane l = kv4_lane(a);
+    if (!l.in) return;
+    for (int r0 = blockIdx.y * RPT; r0 < a.n; r0 += gridDim.y * RPT) {
+        unsigned code[RPT], b[RPT];
+        int slot[RPT];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = kv4_value(code >> (4 * e), scale);
-    T* o = (T*)(kv ? a.v : a.k) + (long long)r * a.row + (long long)h * a.head + piece * 8;
-    if constexpr (sizeof(T) == 4) { *(float4*)o = make_float4(x[0], x[1], x[2], x[3]); *(float4*)(o + 4) = make_float4(x[4], x[5], x[6], x[7]); }
-    else {
-        unsigned u[4];                                      // (exact: two significant bits)
+        for (int u = 0; u < RPT; ++u) slot[u] = kv4_slot(a, r0 + u);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) u[e] = __float_as_uint(x[2 * e]) >> 16 | (__float_as_uint(x[2 * e + 1]) & 0xffff0000u);
-        *(uint4*)o = make_uint4(u[0], u[1], u[2], u[3]);
+        for (int u = 0; u < RPT; ++u) {
+            const Kv4Place p = kv4_place(a.d, a.pool, max(slot[u], 0), l);
+            code[u] = *(const unsigned*)p.code; b[u] = *p.scale;
+        }
+#pragma unroll
+        for (int u = 0; u < RPT; ++u) {
+            if (slot[u] < 0) continue;
+            const float scale = b[u] == 255 ? __uint_as_float(0x7fc00000u) : __uint_as_float(b[u] << 23);
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = kv4_value(code[u] >> (4 * e), scale);
+            T* o = (T*)(l.kv ? a.v : a.k) + (long long)(r0 + u) * a.row + l.at;
+            if constexpr (sizeof(T) == 4) { *(float4*)o = make_float4(x[0], x[1], x[2], x[3]); *(float4*)(o + 4) = make_float4(x[4], x[5], x[6], x[7]); }
+            else {
+                unsigned w[4];                               // (exact: two significant bits)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(x[2 * e]) >> 16 | (__float_as_uint(x[2 * e + 1]) & 0xffff0000u);
+                *(uint4*)o = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+        }
     }
 }
 

@@ -89,21 +89,35 @@ int kv4_plan_launch(hipStream_t st, PlanArgs a) {
     return HIVIS_OK;
 }
 
-static dim3 rows_grid(const RowsArgs& a) { return dim3((unsigned)(((long long)a.n * a.d.heads * 2 * (a.d.hd / 8) + 255) / 256)); }
+// Four rows per thread where that leaves two workgroups to a CU, one where there are fewer (32 rows of 40 heads: latency)
+static bool rows_by_four(const RowsArgs& a, dim3* grid) {
+    const unsigned x = (unsigned)((2LL * a.d.heads * (a.d.hd / 8) + 255) / 256);
+    const bool four = (long long)x * (a.n / 4) >= 512;
+    *grid = dim3(x, (unsigned)std::min(65535, four ? (a.n + 3) / 4 : a.n));
+    return four;
+}
 
 int kv4_append_launch(hipStream_t st, int type, const RowsArgs& a) {
     if (a.n == 0) return HIVIS_OK;
-    if (type == KV4_ROWS_F32) hipLaunchKernelGGL(kv4_append_kernel<float>, rows_grid(a), dim3(256), 0, st, a);
-    else if (type == KV4_ROWS_BF16) hipLaunchKernelGGL(kv4_append_kernel<__bf16>, rows_grid(a), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(kv4_append_kernel<Kv4Halves>, rows_grid(a), dim3(256), 0, st, a);
+    dim3 grid;
+    const bool four = rows_by_four(a, &grid);
+#define KV4_APPEND(T_) do { if (four) hipLaunchKernelGGL((kv4_append_kernel<T_, 4>), grid, dim3(256), 0, st, a); else hipLaunchKernelGGL((kv4_append_kernel<T_, 1>), grid, dim3(256), 0, st, a); } while (0)
+    if (type == KV4_ROWS_F32) KV4_APPEND(float);
+    else if (type == KV4_ROWS_BF16) KV4_APPEND(__bf16);
+    else KV4_APPEND(Kv4Halves);
+#undef KV4_APPEND
     OP_TRY(hipGetLastError());
     return HIVIS_OK;
 }
 
 int kv4_read_launch(hipStream_t st, int type, const RowsArgs& a) {
     if (a.n == 0) return HIVIS_OK;
-    if (type == KV4_ROWS_F32) hipLaunchKernelGGL(kv4_read_kernel<float>, rows_grid(a), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(kv4_read_kernel<__bf16>, rows_grid(a), dim3(256), 0, st, a);
+    dim3 grid;
+    const bool four = rows_by_four(a, &grid);
+#define KV4_READ(T_) do { if (four) hipLaunchKernelGGL((kv4_read_kernel<T_, 4>), grid, dim3(256), 0, st, a); else hipLaunchKernelGGL((kv4_read_kernel<T_, 1>), grid, dim3(256), 0, st, a); } while (0)
+    if (type == KV4_ROWS_F32) KV4_READ(float);
+    else KV4_READ(__bf16);
+#undef KV4_READ
     OP_TRY(hipGetLastError());
     return HIVIS_OK;
 }
