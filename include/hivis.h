@@ -96,6 +96,15 @@ typedef struct {
  * Errors: HIVIS_EINVAL, HIVIS_EHIP (then *out is NULL). */
 int hivis_create(const hivis_config *cfg, const hivis_weights *w, void *hip_stream, hivis_ctx **out);
 
+/* hivis_create with the target cache held in 4 bits (the format below): pools of n_blocks blocks of block_tokens rows per
+ * layer, shared by the sequences, instead of max_vis + max_text rows for each; a cached value takes 0.53 bytes instead of 4.
+ * n_blocks = 0: as many as all sequences can fill.  Every pass (prefill, verify, draft-tree verify) plans its blocks on the
+ * GPU, appends its keys and values and attends to what is held, its own rows among it, so a row is treated alike whichever pass
+ * made it.  The drafter's text-only cache stays as it is; all calls are the same.  Beyond hivis_create's errors: EINVAL for
+ * block_tokens not 16, 32, 64, 128 or 256, or n_blocks < 0; a call whose rows need more blocks than there are returns
+ * HIVIS_ECAP and leaves the context as it was. */
+int hivis_create_kv4(const hivis_config *cfg, const hivis_weights *w, void *hip_stream, int32_t block_tokens, int32_t n_blocks, hivis_ctx **out);
+
 /* Free everything the context owns.  NULL is accepted. */
 int hivis_destroy(hivis_ctx *ctx);
 
@@ -243,8 +252,8 @@ int hivis_tree_accept_sample(hivis_ctx *ctx, float temperature, const float *u, 
  * They need no context.  All pointers are device memory of the current device (EINVAL for anything else), work is only
  * enqueued on hip_stream (a hipStream_t, NULL = default), nothing is allocated, and the calls may be captured into a graph.
  * After a failure hivis_last_error(NULL) has the message (per host thread) and nothing was enqueued.
- * Workspaces belong to the caller: zero-filled once before their first use, left ready for the next call by every call,
- * never used by two calls that may run at the same time (two streams, two graphs replayed side by side: two workspaces).
+ * Workspaces belong to the caller: zero-filled once before their first use, left ready for the next call by every call
+ * (of any sizes that fit, and of either operator), never used by two calls that may run at the same time (two streams, two graphs replayed side by side: two workspaces).
  *
  * The cache is a pool of blocks of block_tokens rows; a sequence's blocks are listed in its row of a block table, and a
  * row's place is its slot = block * block_tokens + offset.  Memory of a block, per key head in order:
@@ -353,6 +362,19 @@ int hivis_tree_get_logits(hivis_ctx *ctx, float *out);
 /* which = 0: logits of the last verify, [B][K+1][vocab] (tree: [n_nodes+1][vocab]); which = 1: logits of the last draft round,
  * [K][B][vocab]; which = 2: logits that chose x_{l+1} at prefill, [B][vocab].  out: float32, host. */
 int hivis_get_logits(hivis_ctx *ctx, int32_t which, float *out);
+
+/* Log probabilities of given tokens under softmax(logits / temperature), entropies and most probable tokens, as
+ * hivis_logprobs, of the rows that hivis_get_logits(which) would copy, without copying them: the tokens a verify pass emitted
+ * with which = 0, the drafts with 1, x_{l+1} with 2.  Host arrays: tokens, logprob [rows][n_tokens] (n_tokens <= 64),
+ * entropy [rows] (may be NULL), top_ids, top_logprobs [rows][top_k] (top_k <= 32).  The first call allocates its buffers.
+ * Errors: ESTATE, EINVAL, EHIP. */
+int hivis_get_logprobs(hivis_ctx *ctx, int32_t which, float temperature, const int32_t *tokens, int32_t n_tokens, float *logprob, float *entropy, int32_t top_k,
+                       int32_t *top_ids, float *top_logprobs);
+
+/* Rows first .. first + n - 1 of a sequence's target cache as held in 4 bits: k, v [n][n_kv_heads][head_dim] float32, host
+ * (after hivis_verify the rows of the pass among them).  The 32 dims of a key that share a scale are 16 rotary pairs
+ * (i, i + head_dim / 2), i = 0..15, 16..31, ...  Errors: ESTATE (not created by hivis_create_kv4), EINVAL, EHIP. */
+int hivis_kv4_get(hivis_ctx *ctx, int32_t layer, int32_t seq, int32_t first, int32_t n, float *k, float *v);
 
 /* which = 0: post-final-norm target features g of the last verify, [B][K+1][d] (tree: [n_nodes+1][d]);
  * which = 1: the drafter's pending hidden state f'_1 for the next round, [B][d].  out: float32, host. */

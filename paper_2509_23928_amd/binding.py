@@ -66,6 +66,7 @@ def load_library(path=LIB_PATH):
     P, I32 = C.c_void_p, C.c_int32
     sig = {
         "hivis_create": (C.c_int, [C.POINTER(hivis_config), C.POINTER(hivis_weights), P, C.POINTER(P)]),
+        "hivis_create_kv4": (C.c_int, [C.POINTER(hivis_config), C.POINTER(hivis_weights), P, I32, I32, C.POINTER(P)]),
         "hivis_destroy": (C.c_int, [P]),
         "hivis_prefill": (C.c_int, [P, P, I32, P, I32, P]),
         "hivis_draft": (C.c_int, [P, I32]),
@@ -86,6 +87,8 @@ def load_library(path=LIB_PATH):
         "hivis_tree_get_logits": (C.c_int, [P, P]),
         "hivis_get_logits": (C.c_int, [P, I32, P]),
         "hivis_get_hidden": (C.c_int, [P, I32, P]),
+        "hivis_get_logprobs": (C.c_int, [P, I32, C.c_float, P, I32, P, P, I32, P, P]),
+        "hivis_kv4_get": (C.c_int, [P, I32, I32, I32, I32, P, P]),
         "hivis_kv_lengths": (C.c_int, [P, P, P]),
         "hivis_get_tokens": (C.c_int, [P, P, P]),
         "hivis_timing": (C.c_int, [P, I32]),
@@ -116,7 +119,7 @@ def load_library(path=LIB_PATH):
 EXPORTED_SYMBOLS = ("hivis_create", "hivis_destroy", "hivis_prefill", "hivis_draft", "hivis_draft_noalloc", "hivis_set_drafts",
                     "hivis_verify", "hivis_accept", "hivis_prefill_sample", "hivis_draft_sample", "hivis_accept_sample", "hivis_rng_seed", "hivis_tree_draft", "hivis_tree_set", "hivis_tree_verify", "hivis_tree_accept", "hivis_tree_accept_sample", "hivis_tree_get", "hivis_tree_get_logits", "hivis_get_logits", "hivis_get_hidden", "hivis_kv_lengths",
                     "hivis_get_tokens", "hivis_timing", "hivis_phase_ms", "hivis_kernel_timing", "hivis_kernel_ms", "hivis_algorithmic_bytes", "hivis_clamp_token", "hivis_calib_stream",
-                    "hivis_kv4_pool_bytes", "hivis_kv4_plan", "hivis_kv4_append", "hivis_kv4_read", "hivis_kv4_attend", "hivis_kv4_attend_bytes", "hivis_logprobs", "hivis_logprobs_bytes",
+                    "hivis_kv4_pool_bytes", "hivis_kv4_plan", "hivis_kv4_append", "hivis_kv4_read", "hivis_kv4_attend", "hivis_kv4_attend_bytes", "hivis_logprobs", "hivis_logprobs_bytes", "hivis_create_kv4", "hivis_get_logprobs", "hivis_kv4_get",
                     "hivis_last_error", "hivis_version")
 
 
@@ -291,7 +294,8 @@ def logprobs(logits, tokens, logprob, entropy=None, top_ids=None, top_logprobs=N
 class Hivis:
     """One library context.  Method names mirror the C entry points."""
 
-    def __init__(self, cfg, weights, *, max_vis=None, max_text=None, k_max=None, batch=None, stream=None):
+    def __init__(self, cfg, weights, *, max_vis=None, max_text=None, k_max=None, batch=None, stream=None, kv4_block=None, kv4_blocks=0):
+        """kv4_block: rows per block of a target cache held in 4 bits (hivis_create_kv4; kv4_blocks: of the pool, 0 = all that can be filled)."""
         self.lib = load_library()
         self.cfg = cfg
         dt = HIVIS_BF16 if cfg.dtype == "bf16" else HIVIS_F32
@@ -317,7 +321,10 @@ class Hivis:
         w = hivis_weights(hw(weights["embed"]), hw(weights["lm_head"]), hw(weights["final_norm"]), layers,
                           layer(weights["draft_layer"]), hw(weights["fuse_w"]), hw(weights["resid_rho"]))
         self.ctx = C.c_void_p()
-        rc = self.lib.hivis_create(C.byref(c), C.byref(w), C.c_void_p(stream or 0), C.byref(self.ctx))
+        if kv4_block is None:
+            rc = self.lib.hivis_create(C.byref(c), C.byref(w), C.c_void_p(stream or 0), C.byref(self.ctx))
+        else:
+            rc = self.lib.hivis_create_kv4(C.byref(c), C.byref(w), C.c_void_p(stream or 0), int(kv4_block), int(kv4_blocks), C.byref(self.ctx))
         if rc:
             raise HivisError(rc, self.lib.hivis_last_error(None).decode())
         self.K = 0
@@ -495,6 +502,22 @@ class Hivis:
         d, B, K = self.cfg.d, self.B, self.K
         shape, rows, written = {0: ((B, K + 1, d), B * (K + 1), self._verify_rows), 1: ((B, d), B, B)}[which]
         return self._read_back(self.lib.hivis_get_hidden, which, shape, rows, written)
+
+    def get_logprobs(self, which, tokens=None, *, temperature=1.0, top_k=0):
+        """hivis_get_logprobs of the rows of get_logits(which) (K of the last chain round, rows of the last verify pass): tokens [rows][n] (None: none).
+        Returns (logprob [rows][n], entropy [rows], top_ids, top_logprobs [rows][top_k])."""
+        rows = {0: self._verify_rows, 1: self._draft_K * self.B, 2: self.B}[which]
+        t = np.zeros((rows, 0), np.int32) if tokens is None else np.ascontiguousarray(tokens, dtype=np.int32).reshape(rows, -1)
+        lp, h = np.zeros(t.shape, np.float32), np.zeros(rows, np.float32)
+        ids, top = np.zeros((rows, top_k), np.int32), np.zeros((rows, top_k), np.float32)
+        self._check(self.lib.hivis_get_logprobs(self.ctx, which, temperature, _ptr(t), t.shape[1], _ptr(lp), _ptr(h), top_k, _ptr(ids), _ptr(top)))
+        return lp, h, ids, top
+
+    def kv4_get(self, layer, seq, first, n):
+        """hivis_kv4_get: keys and values [n][n_kv_heads][head_dim] of the target cache as held in 4 bits."""
+        k, v = (np.zeros((n, self.cfg.n_kv_heads, self.cfg.head_dim), np.float32) for _ in range(2))
+        self._check(self.lib.hivis_kv4_get(self.ctx, layer, seq, first, n, _ptr(k), _ptr(v)))
+        return k, v
 
     def kv_lengths(self):
         t = np.zeros(self.B, np.int32)

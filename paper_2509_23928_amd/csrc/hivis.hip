@@ -9,6 +9,8 @@
 #include "hivis_tile.h"
 #include "hivis_attn.h"
 #include "hivis_tree.h"
+#include "hivis_kv4_args.h"
+#include "hivis_logprobs_args.h"
 #include "hivis_ops.h"
 
 #include <hip/hip_ext.h>
@@ -48,7 +50,9 @@ struct LayerDev {
     float* bqkv = nullptr;                          // optional q/k/v projection biases [q_dim + 2 kv_dim], in wqkv's column order
 };
 
-struct KVDev { void* k = nullptr; void* v = nullptr; int maxL = 0; };   // [B][Hkv][maxL][hd]
+// [B][Hkv][maxL][hd].  kv4: 1 + target layer of a context whose target cache is held in 4 bits; k and v are then the rows of the pass at hand, shared by all
+// layers, at their positions: what the q|k|v kernels write there goes to the layer's pool before the attention
+struct KVDev { void* k = nullptr; void* v = nullptr; int maxL = 0; int kv4 = 0; };
 
 }  // namespace
 
@@ -136,6 +140,13 @@ struct hivis_ctx {
     // passes that no phase program takes: split-K layers from wide_min rows on (with stand-alone kernels on both sides 10 rows were faster
     // on the skinny ones, 12 on the split-K layer); HIVIS_WIDE_GEMM=0: never
     bool no_wide_gemm = false; int wide_min = 11;
+    // target cache in 4 bits (hivis_create_kv4): pools of the layers, one after the other; tables and slots of the pass at hand (kv4_rows rows per sequence)
+    bool kv4 = false; Kv4Dims kv4_dims{}; long long kv4_pool = 0; uint8_t* kv4_mem = nullptr;
+    int kv4_max_blocks = 0, kv4_rows = 0;
+    int *kv4_table = nullptr, *kv4_free = nullptr, *kv4_held = nullptr, *kv4_start = nullptr, *kv4_slots = nullptr, *kv4_status = nullptr;
+    void* kv4_ws = nullptr;
+    // hivis_get_logprobs: tokens, results and workspace, allocated by the first call
+    int32_t *lp_tokens = nullptr, *lp_ids = nullptr; float *lp_out = nullptr, *lp_entropy = nullptr, *lp_top = nullptr; void* lp_ws = nullptr;
     int32_t* h_tree_result = nullptr;                     // pinned [1 + TREE_MAX_DEPTH + 1]
 
     // timing
@@ -171,7 +182,7 @@ int fail(hivis_ctx* c, int code, const char* fmt, ...) {
 
 // Device address of the static scratch array on device `dev` (which must be the current device): looked up once per
 // device, then kept for the life of the process.
-constexpr int MAX_DEVICES = 64;
+constexpr int MAX_DEVICES = 64, GET_LOGPROBS_TOKENS = 64;
 void* g_scratch_ptr[MAX_DEVICES] = {};
 std::mutex g_scratch_mu;
 int scratch_for_device(hivis_ctx* c, int dev) {
@@ -333,9 +344,13 @@ int gemm(hivis_ctx* c, const float* A, int lda, int M, int K, const uint4* Wp, i
     return HIVIS_OK;
 }
 
+int kv4_attention(hivis_ctx* c, const KVDev& kv, const float* q, int ldq, const int* base, int offset, int seq0, int nseq, int m, int qrows, float* out, int ldo,
+                  const unsigned long long* tmask);
+
 template <typename WT>
 int attention(hivis_ctx* c, const float* q, int ldq, const KVDev& kv, const int* base, int offset, int seq0, int nseq,
               int m, int max_keys, float* out, int ldo, const unsigned long long* tmask = nullptr, int qrows = 0) {
+    if (kv.kv4) return kv4_attention(c, kv, q, ldq, base, offset, seq0, nseq, m, qrows, out, ldo, tmask);
     typedef typename KVType<WT>::type KT;
     const hivis_config& g = c->cfg;
     AttnShape sh{};
@@ -377,6 +392,48 @@ int attention(hivis_ctx* c, const float* q, int ldq, const KVDev& kv, const int*
 }
 
 AttnShape fused_attn_shape(hivis_ctx* c, int nseq, int m, int offset, int maxL, int ldq, bool alone, int* items_out);
+
+// ---- target cache in 4 bits ----
+// Tables and slots of a pass over `add` new rows of every sequence behind the first keep[b] (null: 0).  The blocks are there: kv4_room has counted them.
+int kv4_pass(hivis_ctx* c, const int* keep, int add) {
+    const hivis_config& g = c->cfg;
+    PlanArgs a{};
+    a.n = g.batch; a.max_blocks = c->kv4_max_blocks; a.shift = c->kv4_dims.shift; a.n_blocks = c->kv4_dims.n_blocks; a.max_rows = g.batch * add;
+    a.keep = keep; a.held = c->kv4_held; a.table = c->kv4_table; a.free_list = c->kv4_free; a.row_start = c->kv4_start; a.slots = c->kv4_slots; a.status = c->kv4_status; a.add_each = add;
+    c->kv4_rows = add;
+    if (int rc = kv4_plan_launch(c->stream, a)) return fail(c, rc, "%s", hivis_last_error(nullptr));
+    return HIVIS_OK;
+}
+
+int kv4_room(hivis_ctx* c, bool empty, int add) {
+    if (!c->kv4) return HIVIS_OK;
+    long long need = 0;
+    for (int b = 0; b < c->cfg.batch; ++b) need += ((empty ? 0 : c->h_tlen[b]) + add + c->kv4_dims.block - 1) / c->kv4_dims.block;
+    if (need > c->kv4_dims.n_blocks) return fail(c, HIVIS_ECAP, "%lld blocks of the target cache needed, %d in the pool", need, c->kv4_dims.n_blocks);
+    return HIVIS_OK;
+}
+
+// Rows of the pass (the last qrows or m of each sequence) to the layer's pool, then attention of the last m rows of each of nseq sequences to fp32 rows
+int kv4_attention(hivis_ctx* c, const KVDev& kv, const float* q, int ldq, const int* base, int offset, int seq0, int nseq, int m, int qrows, float* out, int ldo,
+                  const unsigned long long* tmask) {
+    const hivis_config& g = c->cfg;
+    const int rows = qrows ? qrows : m, start = offset + m - rows;       // of the pass, per sequence: its first row behind base
+    RowsArgs r{};
+    r.d = c->kv4_dims; r.row = g.head_dim; r.head = (long long)kv.maxL * g.head_dim; r.seq = g.n_kv_heads * r.head;
+    const size_t at = (size_t)seq0 * r.seq * (g.dtype == HIVIS_BF16 ? KVWidth<f16_t>::W * sizeof(f16_t) : sizeof(float));
+    r.k = (const char*)kv.k + at; r.v = (const char*)kv.v + at; r.n = nseq * rows; r.slots = c->kv4_slots + (size_t)seq0 * c->kv4_rows + start;
+    r.pool = c->kv4_mem + (kv.kv4 - 1) * c->kv4_pool; r.first = base + seq0; r.m = rows; r.offset = start;
+    if (int rc = kv4_append_launch(c->stream, g.dtype == HIVIS_BF16 ? KV4_ROWS_HALVES : KV4_ROWS_F32, r)) return fail(c, rc, "%s", hivis_last_error(nullptr));
+    Kv4AttnArgs a{};
+    a.d = c->kv4_dims; a.group = g.n_q_heads / g.n_kv_heads; a.n_seqs = nseq; a.n_rows = nseq * m; a.max_blocks = c->kv4_max_blocks;
+    a.scale2 = (float)(1.4426950408889634 / std::sqrt((double)g.head_dim));
+    a.pool = r.pool; a.table = c->kv4_table; a.kv_len = base; a.q = q; a.ldq = ldq; a.mask = tmask; a.out = out; a.ldo = ldo;
+    a.m = m; a.qrows = rows; a.seq0 = seq0; a.len_add = offset + m;
+    int keys = 0;
+    if (base == c->tlen) for (int s = 0; s < nseq; ++s) keys = std::max(keys, c->h_tlen[seq0 + s]);
+    if (int rc = kv4_attend_launch(c->stream, HIVIS_F32, a, m, keys + offset + m, c->kv4_ws)) return fail(c, rc, "%s", hivis_last_error(nullptr));
+    return HIVIS_OK;
+}
 
 int key_splits(const hivis_ctx* c, int keys, int most, bool half) { return half && !c->keys_forced ? attn_block_splits(keys, most) : attn_splits(keys, most, c->keys_per_split); }
 
@@ -430,6 +487,14 @@ int attention_rows_mfma(hivis_ctx* c, const float* q, int ldq, const KVDev& kv, 
     // (K = ldo) instead of fp32 rows, and *wrote_frag says so
     if (wrote_frag) *wrote_frag = false;
     const hivis_config& g = c->cfg;
+    if (kv.kv4) {
+        // (its kernels write fp32 rows; row fragments take a launch of their own)
+        float* rows = row_frag ? c->pf_att : out;
+        if (int rc = kv4_attention(c, kv, q, ldq, base, offset, seq0, nseq, m, qrows, rows, ldo, tmask)) return rc;
+        if (row_frag) hipLaunchKernelGGL(stream_rows_kernel, dim3(nseq * m), dim3(FUSED_NT), 0, c->stream, (const float*)rows, ldo, ldo, (const bf16_t*)nullptr, row_frag, 0, nseq * m, (float*)nullptr);
+        HIP_TRY(c, hipGetLastError());
+        return HIVIS_OK;
+    }
     typedef typename KVType<WT>::type KT;
     if constexpr (std::is_same<KT, f16_t>::value) {
         // long causal row ranges (prefill): key tiles shared by a workgroup through LDS.  Too few such workgroups leave CUs idle
@@ -645,7 +710,7 @@ float* layer_phases(hivis_ctx* c, std::vector<Phase>& P, Pool& pool, const Layer
     Phase q{}; q.type = PH_GEMM; q.pro = PRO_RMS; q.epi = FEPI_QKV; q.K = d; q.N = nqkv; q.W = L.wqkv; q.A = h; q.lda = d;
     q.gain = L.norm1; q.Y = qkv; q.ldy = nqkv; q.kc = kv.k; q.vc = kv.v; q.maxL = kv.maxL; q.base = base; q.offset = offset; q.rope = c->rope_tab; q.bias = L.bqkv;
     P.push_back(q);
-    Phase a{}; a.type = PH_ATTN; a.A = qkv; a.lda = nqkv; a.kc = kv.k; a.vc = kv.v; a.maxL = kv.maxL; a.base = base; a.offset = offset;
+    Phase a{}; a.type = PH_ATTN; a.A = qkv; a.lda = nqkv; a.kc = kv.k; a.vc = kv.v; a.maxL = kv.maxL; a.base = base; a.offset = offset; a.K = kv.kv4;
     a.att = fused_attn_shape(c, nseq, m, offset, kv.maxL, nqkv, false, &a.att_items);
     int items = a.att_items;                           // (of the launch with the most, and the most partials)
     if (alone) { (void)fused_attn_shape(c, nseq, m, offset, kv.maxL, nqkv, true, &items); a.att_alone = items > a.att_items; }
@@ -695,7 +760,7 @@ void layer_stream(hivis_ctx* c, std::vector<Phase>& P, Pool& pool, const LayerDe
     q.gain = L.norm1; q.Y = qrows; q.ldy = qd; q.kc = kv.k; q.vc = kv.v; q.maxL = kv.maxL; q.base = base; q.offset = offset; q.rope = c->rope_tab; q.bias = L.bqkv;
     q.Af = in.F; q.ssq = in.ssq; q.nssq = in.nssq;
     P.push_back(q);
-    Phase a{}; a.type = PH_ATTN; a.A = qrows; a.lda = qd; a.kc = kv.k; a.vc = kv.v; a.maxL = kv.maxL; a.base = base; a.offset = offset;
+    Phase a{}; a.type = PH_ATTN; a.A = qrows; a.lda = qd; a.kc = kv.k; a.vc = kv.v; a.maxL = kv.maxL; a.base = base; a.offset = offset; a.K = kv.kv4;
     a.att = fused_attn_shape(c, nseq, m, offset, kv.maxL, qd, false, &a.att_items);
     a.ws = pool.take(attn_partials(c->fused_grid, a.att_items) * FUSED_RMAX * (g.head_dim + 2));
     a.F = attF; a.ldy = qd;
@@ -959,6 +1024,15 @@ int launch_phases(hivis_ctx* c, const Phase* phases, int n, int kind, int K, con
     const bool keep = !std::is_same<WT, float>::value && (kind == PROG_DRAFT || kind == PROG_DRAFT_SAMPLE) && K > 1 && g.d <= STREAM_SHORT_K && draft_step_bytes(c) <= 256.0e6;
     for (int p = 0; p < n; ++p) {
         Phase ph = phases[p];
+        if (ph.type == PH_ATTN_MERGE && ph.K) continue;
+        if (ph.type == PH_ATTN && ph.K) {          // a target layer of a context whose cache is held in 4 bits
+            KVDev kv; kv.k = ph.kc; kv.v = ph.vc; kv.maxL = ph.maxL; kv.kv4 = ph.K;
+            float* rows = ph.F ? c->att : ph.Y;
+            const int ld = ph.F ? g.n_q_heads * g.head_dim : ph.ldy;
+            if (int rc = kv4_attention(c, kv, ph.A, ph.lda, ph.base, ph.offset, 0, pp.nseq, pp.m, 0, rows, ld, ph.att.tmask)) return rc;
+            if (ph.F) hipLaunchKernelGGL(stream_rows_kernel, dim3(pp.M), dim3(FUSED_NT), 0, c->stream, (const float*)rows, ld, ld, (const bf16_t*)nullptr, ph.F, 0, pp.M, (float*)nullptr);
+            continue;
+        }
         ph.next_W = nullptr;                       // nothing is prefetched across a kernel boundary (pulling the next launch's
                                                    // first units into L2 during the epilogue was measured: 3% slower)
         if (ph.type == PH_ATTN || ph.type == PH_ATTN_MERGE) {
@@ -1728,6 +1802,7 @@ int do_prefill(hivis_ctx* c, const void* vis_embeds, int v, const int32_t* text_
     if (c->bar) hipLaunchKernelGGL(set_ints_kernel, dim3(1), dim3(64), 0, c->stream, (int*)c->bar, 2, 0);
 
     const int total = v + l;
+    if (c->kv4) if (int rc = kv4_pass(c, nullptr, total)) return rc;
     // bf16 models: whole prompts, as many sequences at a time as the buffers hold; fp32: chunks of the decode passes' size
     [[maybe_unused]] const int per = std::max(1, std::min(B, c->pf_rows / total));
     if constexpr (sizeof(WT) == 2) {
@@ -1817,6 +1892,7 @@ int do_verify(hivis_ctx* c) {
     PhaseTimer pt(c, 2);
     int max_keys = 0;
     for (int b = 0; b < B; ++b) max_keys = std::max(max_keys, c->h_tlen[b]);
+    if (c->kv4) if (int rc = kv4_pass(c, c->tlen, K + 1)) return rc;
     hipLaunchKernelGGL(verify_tokens_kernel, dim3(1), dim3(64), 0, c->stream, (const int32_t*)c->text, c->text_stride, (const int*)c->dlen, (const int32_t*)c->drafts, g.k_max, K, c->row_tok, B);
     if (c->fused && fused_rows_ok<WT>(c, M)) {
         if (int rc = run_program<WT>(c, PROG_VERIFY, K, B, K + 1)) return rc;
@@ -2073,6 +2149,7 @@ int do_tree_verify(hivis_ctx* c) {
     const int d = g.d, V = g.vocab, M = c->tn + 1;
     PhaseTimer pt(c, 2);
     const TreeDev& t = c->tree;
+    if (c->kv4) if (int rc = kv4_pass(c, c->tlen, M)) return rc;
     hipLaunchKernelGGL((gather_rows_kernel<WT>), dim3(M), dim3(256), 0, c->stream, (const WT*)c->embed, (const int32_t*)t.row_tok, M, 0, c->x, d, d);
     TreeRows tr; tr.pos_delta = t.row_depth; tr.mask = t.vmask;
     if (int rc = target_forward<WT>(c, 0, 1, M, c->tlen, 0, c->h_tlen[0] + M, c->catT, 2 * d, 0, tr)) return rc;
@@ -2097,7 +2174,9 @@ int do_tree_accept(hivis_ctx* c, int32_t* n_accepted, int32_t* tokens, bool samp
                                    (const float*)c->u_tree, 1, t.ttok, 1, (const int32_t*)t.row_depth);
     hipLaunchKernelGGL(tree_accept_kernel, dim3(1), dim3(64), 0, c->stream, N, depth, c->text, (const int*)c->dlen, t);
     // target cache: the followed rows move to the slots right after the root's
-    for (int scatter = 0; scatter < 2; ++scatter)
+    if (c->kv4) {
+        if (int rc = kv4_move_launch(c->stream, c->kv4_dims, c->kv4_mem, c->kv4_pool, g.n_layers, c->kv4_table, c->tlen, t.result, t.path, depth)) return fail(c, rc, "%s", hivis_last_error(nullptr));
+    } else for (int scatter = 0; scatter < 2; ++scatter)
         hipLaunchKernelGGL((tree_kv_gather_kernel<KT>), dim3(depth, 2 * g.n_layers), dim3(256), 0, c->stream, (KT* const*)c->kv_ptrs, c->tkv[0].maxL,
                            g.n_kv_heads, g.head_dim * KVWidth<KT>::W, (const int*)c->tlen, (const int32_t*)t.result, (const int32_t*)t.path, depth, (KT*)c->kv_staging, scatter);
     // drafter: every tree row is dropped (its length never advanced); depth+1 rows rebuilt from the true features
@@ -2185,6 +2264,30 @@ int build_embed_fc_table(hivis_ctx* c, const hivis_weights* w) {
     return rc;
 }
 
+// Pools, tables and workspace of a target cache in 4 bits (dims are set)
+int kv4_setup(hivis_ctx* c) {
+    const hivis_config& g = c->cfg;
+    const Kv4Dims& d = c->kv4_dims;
+    const int B = g.batch, cap = g.max_vis + g.max_text, most = std::max(cap, MAX_ROWS);
+    c->kv4_pool = (long long)d.n_blocks * d.heads * kv4_chunk(d.hd, d.block);
+    c->kv4_max_blocks = (cap + d.block - 1) / d.block;
+    int rc;
+    unsigned char* ws;
+    const long long space = kv4_stream_space(d.hd);
+    if ((rc = dev_alloc(c, &c->kv4_mem, (size_t)c->kv4_pool * g.n_layers)) || (rc = dev_alloc(c, &c->kv4_table, (size_t)B * c->kv4_max_blocks)) || (rc = dev_alloc(c, &c->kv4_free, (size_t)d.n_blocks + 1)) ||
+        (rc = dev_alloc(c, &c->kv4_held, B)) || (rc = dev_alloc(c, &c->kv4_start, B + 1)) || (rc = dev_alloc(c, &c->kv4_slots, (size_t)B * most)) || (rc = dev_alloc(c, &c->kv4_status, B)) ||
+        (rc = dev_alloc(c, &ws, (size_t)space))) return rc;
+    c->kv4_ws = ws;
+    std::vector<int> list(d.n_blocks + 1);
+    list[0] = d.n_blocks;
+    for (int i = 0; i < d.n_blocks; ++i) list[1 + i] = d.n_blocks - 1 - i;         // (the first block is taken first)
+    HIP_TRY(c, hipMemcpy(c->kv4_free, list.data(), list.size() * sizeof(int), hipMemcpyHostToDevice));
+    HIP_TRY(c, hipMemset(c->kv4_held, 0, B * sizeof(int)));
+    HIP_TRY(c, hipMemset(c->kv4_table, 0xff, (size_t)B * c->kv4_max_blocks * sizeof(int)));
+    HIP_TRY(c, hipMemset(c->kv4_ws, 0, (size_t)space));
+    return HIVIS_OK;
+}
+
 template <typename WT>
 int do_create(hivis_ctx* c, const hivis_weights* w) {
     const hivis_config& g = c->cfg;
@@ -2216,10 +2319,12 @@ int do_create(hivis_ctx* c, const hivis_weights* w) {
     c->tkv.resize(g.n_layers);
     for (int l = 0; l < g.n_layers; ++l) {
         typename KVType<WT>::type *k, *v;
+        if (c->kv4 && l > 0) { c->tkv[l] = c->tkv[0]; c->tkv[l].kv4 = l + 1; continue; }
         if ((rc = dev_alloc(c, &k, (size_t)B * kd * maxLt * KW))) return rc;
         if ((rc = dev_alloc(c, &v, (size_t)B * kd * maxLt * KW))) return rc;
-        c->tkv[l].k = k; c->tkv[l].v = v; c->tkv[l].maxL = maxLt;
+        c->tkv[l].k = k; c->tkv[l].v = v; c->tkv[l].maxL = maxLt; c->tkv[l].kv4 = c->kv4;
     }
+    if (c->kv4 && (rc = kv4_setup(c))) return rc;
     { typename KVType<WT>::type *k, *v;
       if ((rc = dev_alloc(c, &k, (size_t)B * kd * maxLd * KW))) return rc;
       if ((rc = dev_alloc(c, &v, (size_t)B * kd * maxLd * KW))) return rc;
@@ -2295,7 +2400,7 @@ int do_create(hivis_ctx* c, const hivis_weights* w) {
     }
     if ((rc = fused_setup<WT>(c))) return rc;
     // (attention rows of a whole-prompt pass: as fragments except from passes of at most 8 rows per sequence, and HIVIS_FUSED=0)
-    if (c->pf_rows && (rc = dev_alloc(c, &c->pf_att, (size_t)(c->fused ? B * FUSED_RMAX : c->pf_rows) * qd))) return rc;
+    if (c->pf_rows && (rc = dev_alloc(c, &c->pf_att, (size_t)(c->fused && !c->kv4 ? B * FUSED_RMAX : c->pf_rows) * qd))) return rc;
     // attention workspace: (items * nsplit) work groups x 4 wave slots x RMAX rows x (hd + 2) floats, where
     // items * nsplit <= 2 * num_cu + items and items <= max(2, B) * n_q_heads
     {
@@ -2352,15 +2457,13 @@ namespace hivis { void set_thread_error(const char* message) { g_create_err = me
 
 extern "C" {
 
-int hivis_create(const hivis_config* cfg, const hivis_weights* w, void* hip_stream, hivis_ctx** out) {
-    if (out) *out = nullptr;
-    if (!cfg || !w || !out) { g_create_err = "null argument"; return HIVIS_EINVAL; }
-    if (int rc = check_config(cfg, g_create_err)) return rc;
+static int create(const hivis_config* cfg, const hivis_weights* w, void* hip_stream, const Kv4Dims* kv4, hivis_ctx** out) {
     if (!w->embed || !w->lm_head || !w->final_norm || !w->layers || !w->fuse_w || !w->resid_rho) { g_create_err = "null weight pointer"; return HIVIS_EINVAL; }
     hivis_ctx* c = new hivis_ctx();
     c->cfg = *cfg;
     c->stream = (hipStream_t)hip_stream;
     c->esize = cfg->dtype == HIVIS_BF16 ? 2 : 4;
+    if (kv4) { c->kv4 = true; c->kv4_dims = *kv4; }
     int dev = 0; hipDeviceProp_t prop;
     if (hipGetDevice(&dev) != hipSuccess || hipGetDeviceProperties(&prop, dev) != hipSuccess) {
         g_create_err = "no HIP device"; delete c; return HIVIS_EHIP;
@@ -2369,9 +2472,30 @@ int hivis_create(const hivis_config* cfg, const hivis_weights* w, void* hip_stre
     c->na_phases.reserve(draft_phase_capacity(cfg->k_max));
     int rc = scratch_for_device(c, dev);
     if (!rc) rc = DISPATCH(c, do_create, c, w);
+    if (!rc && c->kv4 && c->persistent) rc = fail(c, HIVIS_EINVAL, "a target cache in 4 bits needs one launch per phase (HIVIS_PERSISTENT not 1)");
     if (rc) { g_create_err = c->err; hivis_destroy(c); return rc; }
     *out = c;
     return HIVIS_OK;
+}
+
+int hivis_create(const hivis_config* cfg, const hivis_weights* w, void* hip_stream, hivis_ctx** out) {
+    if (out) *out = nullptr;
+    if (!cfg || !w || !out) { g_create_err = "null argument"; return HIVIS_EINVAL; }
+    if (int rc = check_config(cfg, g_create_err)) return rc;
+    return create(cfg, w, hip_stream, nullptr, out);
+}
+
+int hivis_create_kv4(const hivis_config* cfg, const hivis_weights* w, void* hip_stream, int32_t block_tokens, int32_t n_blocks, hivis_ctx** out) {
+    if (out) *out = nullptr;
+    if (!cfg || !w || !out) { g_create_err = "null argument"; return HIVIS_EINVAL; }
+    if (int rc = check_config(cfg, g_create_err)) return rc;
+    const long long cap = (long long)cfg->max_vis + cfg->max_text, each = block_tokens > 0 ? (cap + block_tokens - 1) / block_tokens : 0;
+    if (n_blocks == 0) n_blocks = (int)std::min<long long>(0x7fffffff, each * cfg->batch);
+    const hivis_kv4_shape shape{cfg->n_kv_heads, cfg->head_dim, block_tokens, n_blocks};
+    const int64_t bytes = hivis_kv4_pool_bytes(&shape);
+    if (bytes < 0) return (int)bytes;
+    const Kv4Dims d{cfg->n_kv_heads, cfg->head_dim, block_tokens, __builtin_ctz(block_tokens), n_blocks};
+    return create(cfg, w, hip_stream, &d, out);
 }
 
 int hivis_destroy(hivis_ctx* c) {
@@ -2392,6 +2516,7 @@ int hivis_prefill(hivis_ctx* c, const void* vis_embeds, int32_t v, const int32_t
     const hivis_config& g = c->cfg;
     if (!text_ids || v < 0 || l < 1 || (v > 0 && !vis_embeds)) return fail(c, HIVIS_EINVAL, "bad prefill arguments (v=%d, l=%d)", v, l);
     if (v > g.max_vis || l + g.k_max + 2 > g.max_text) return fail(c, HIVIS_ECAP, "prompt exceeds capacity (v=%d/%d, l=%d/%d)", v, g.max_vis, l, g.max_text);
+    if (int rc = kv4_room(c, true, v + l)) return rc;
     c->h_ids.resize((size_t)g.batch * l);
     HIP_TRY(c, hipMemcpy(c->h_ids.data(), text_ids, c->h_ids.size() * sizeof(int32_t), hipMemcpyDefault));
     for (int32_t id : c->h_ids)
@@ -2429,6 +2554,7 @@ int hivis_prefill_sample(hivis_ctx* c, const void* vis_embeds, int32_t v, const 
     if (!u_first && !c->rng_seeded) return fail(c, HIVIS_ESTATE, "null u_first needs hivis_rng_seed first");
     if (u_first) { if (int rc = check_uniforms(c, u_first, (size_t)g.batch, "u_first")) return rc; }
     if (v > g.max_vis || l + g.k_max + 2 > g.max_text) return fail(c, HIVIS_ECAP, "prompt exceeds capacity (v=%d/%d, l=%d/%d)", v, g.max_vis, l, g.max_text);
+    if (int rc = kv4_room(c, true, v + l)) return rc;
     c->h_ids.resize((size_t)g.batch * l);
     HIP_TRY(c, hipMemcpy(c->h_ids.data(), text_ids, c->h_ids.size() * sizeof(int32_t), hipMemcpyDefault));
     for (int32_t id : c->h_ids)
@@ -2446,7 +2572,7 @@ static int check_room(hivis_ctx* c, int K) {
         if (c->h_dlen[b] + K + 2 > g.max_text) return fail(c, HIVIS_ECAP, "sequence %d: text length %d + K + 2 exceeds max_text %d", b, c->h_dlen[b], g.max_text);
         if (c->h_tlen[b] + K + 1 > g.max_vis + g.max_text) return fail(c, HIVIS_ECAP, "sequence %d: target cache full", b);
     }
-    return HIVIS_OK;
+    return kv4_room(c, false, K + 1);
 }
 
 int hivis_draft(hivis_ctx* c, int32_t K) {
@@ -2562,6 +2688,7 @@ int hivis_tree_draft(hivis_ctx* c, int32_t top_k, int32_t depth, int32_t n_nodes
     if (n_nodes < 1 || n_nodes > P || n_nodes + 1 > TREE_MAX_ROWS) return fail(c, HIVIS_EINVAL, "n_nodes=%d outside [1, min(pool %d, %d)]", n_nodes, P, TREE_MAX_ROWS - 1);
     if (c->h_dlen[0] + std::max((depth - 1) * top_k, depth + 1) + 2 > g.max_text) return fail(c, HIVIS_ECAP, "text length %d + tree rows exceeds max_text %d", c->h_dlen[0], g.max_text);
     if (c->h_tlen[0] + n_nodes + 1 > g.max_vis + g.max_text) return fail(c, HIVIS_ECAP, "target cache full");
+    if (int rc = kv4_room(c, false, n_nodes + 1)) return rc;
     int rc = DISPATCH(c, do_tree_draft, c, top_k, depth, n_nodes);
     if (rc) return rc;
     c->tk = top_k; c->tdepth = depth; c->tn = n_nodes; c->state = ST_TREE_DRAFTED;
@@ -2588,6 +2715,7 @@ int hivis_tree_set(hivis_ctx* c, int32_t n_nodes, const int32_t* tokens, const i
     if (depth > TREE_MAX_DEPTH) return fail(c, HIVIS_EINVAL, "planted tree depth %d > %d", depth, TREE_MAX_DEPTH);
     if (c->h_dlen[0] + depth + 3 > g.max_text) return fail(c, HIVIS_ECAP, "text length %d + tree rows exceeds max_text %d", c->h_dlen[0], g.max_text);
     if (c->h_tlen[0] + n_nodes + 1 > g.max_vis + g.max_text) return fail(c, HIVIS_ECAP, "target cache full");
+    if (int rc = kv4_room(c, false, n_nodes + 1)) return rc;
     if (int rc = DISPATCH(c, tree_setup, c)) return rc;
     const TreeDev& t = c->tree;
     // row 0's token: the last known text token (device to device)
@@ -2689,6 +2817,85 @@ int hivis_get_hidden(hivis_ctx* c, int32_t which, float* out) {
     return HIVIS_OK;
 }
 
+int hivis_get_logprobs(hivis_ctx* c, int32_t which, float temperature, const int32_t* tokens, int32_t n_tokens, float* logprob, float* entropy, int32_t top_k, int32_t* top_ids,
+                       float* top_logprobs) {
+    if (!c) return HIVIS_EINVAL;
+    const hivis_config& g = c->cfg;
+    const float inv = 1.f / temperature;
+    if (c->state == ST_CREATED) return fail(c, HIVIS_ESTATE, "nothing computed yet");
+    if (!(temperature > 0.f) || !(inv > 0.f) || !std::isfinite(inv)) return fail(c, HIVIS_EINVAL, "temperature %g: it and its reciprocal must be positive and finite", (double)temperature);
+    if (n_tokens < 0 || n_tokens > GET_LOGPROBS_TOKENS || (n_tokens && (!tokens || !logprob))) return fail(c, HIVIS_EINVAL, "n_tokens=%d outside [0,%d], or null", n_tokens, GET_LOGPROBS_TOKENS);
+    if (top_k < 0 || top_k > std::min(LOGPROBS_MAX_TOP, g.vocab) || (top_k && (!top_ids || !top_logprobs))) return fail(c, HIVIS_EINVAL, "top_k=%d outside [0,%d], or null", top_k, std::min(LOGPROBS_MAX_TOP, g.vocab));
+    const float* src; int rows;
+    if (which == 0) {
+        if ((c->state != ST_VERIFIED && c->state != ST_TREE_VERIFIED && c->state != ST_READY) || c->vrows < 1) return fail(c, HIVIS_ESTATE, "no verify logits");
+        src = c->logits_v; rows = c->vrows;
+    } else if (which == 1) { src = c->logits_d; rows = c->K * g.batch; if (rows < 1) return fail(c, HIVIS_ESTATE, "no draft round yet"); }
+    else if (which == 2) { src = c->logits_p; rows = g.batch; }
+    else return fail(c, HIVIS_EINVAL, "which=%d", which);
+    if (!c->lp_ws) {
+        const int most = std::max(MAX_ROWS, g.k_max * g.batch);
+        long long space = 0;
+        for (int r = 1; r <= most; ++r) space = std::max(space, logprobs_space(r, g.vocab, std::min(LOGPROBS_MAX_TOP, g.vocab)));
+        unsigned char* ws;
+        int rc;
+        if ((rc = dev_alloc(c, &c->lp_tokens, (size_t)most * GET_LOGPROBS_TOKENS)) || (rc = dev_alloc(c, &c->lp_out, (size_t)most * GET_LOGPROBS_TOKENS)) || (rc = dev_alloc(c, &c->lp_entropy, most)) ||
+            (rc = dev_alloc(c, &c->lp_ids, (size_t)most * LOGPROBS_MAX_TOP)) || (rc = dev_alloc(c, &c->lp_top, (size_t)most * LOGPROBS_MAX_TOP)) || (rc = dev_alloc(c, &ws, (size_t)space))) return rc;
+        HIP_TRY(c, hipMemsetAsync(ws, 0, (size_t)space, c->stream));
+        c->lp_ws = ws;
+    }
+    if (n_tokens) HIP_TRY(c, hipMemcpyAsync(c->lp_tokens, tokens, (size_t)rows * n_tokens * sizeof(int32_t), hipMemcpyHostToDevice, c->stream));
+    LogprobsArgs a{};
+    a.x = src; a.ld = g.vocab; a.rows = rows; a.vocab = g.vocab; a.inv_temp = inv; a.tokens = c->lp_tokens; a.n_tokens = n_tokens; a.logprob = c->lp_out; a.entropy = entropy ? c->lp_entropy : nullptr;
+    a.top = top_k; a.top_ids = c->lp_ids; a.top_logprobs = c->lp_top;
+    if (int rc = logprobs_launch(c->stream, HIVIS_F32, a, c->lp_ws)) return fail(c, rc, "%s", hivis_last_error(nullptr));
+    if (n_tokens) HIP_TRY(c, hipMemcpyAsync(logprob, c->lp_out, (size_t)rows * n_tokens * sizeof(float), hipMemcpyDeviceToHost, c->stream));
+    if (entropy) HIP_TRY(c, hipMemcpyAsync(entropy, c->lp_entropy, (size_t)rows * sizeof(float), hipMemcpyDeviceToHost, c->stream));
+    if (top_k) {
+        HIP_TRY(c, hipMemcpyAsync(top_ids, c->lp_ids, (size_t)rows * top_k * sizeof(int32_t), hipMemcpyDeviceToHost, c->stream));
+        HIP_TRY(c, hipMemcpyAsync(top_logprobs, c->lp_top, (size_t)rows * top_k * sizeof(float), hipMemcpyDeviceToHost, c->stream));
+    }
+    HIP_TRY(c, hipStreamSynchronize(c->stream));
+    return HIVIS_OK;
+}
+
+int hivis_kv4_get(hivis_ctx* c, int32_t layer, int32_t seq, int32_t first, int32_t n, float* k, float* v) {
+    if (!c) return HIVIS_EINVAL;
+    const hivis_config& g = c->cfg;
+    if (!c->kv4) return fail(c, HIVIS_ESTATE, "the target cache is not held in 4 bits (hivis_create_kv4)");
+    if (c->state == ST_CREATED) return fail(c, HIVIS_ESTATE, "nothing computed yet");
+    if (layer < 0 || layer >= g.n_layers || seq < 0 || seq >= g.batch || !k || !v) return fail(c, HIVIS_EINVAL, "layer %d, sequence %d, or null", layer, seq);
+    const int held = c->h_tlen[seq] + (c->state == ST_VERIFIED ? c->K + 1 : c->state == ST_TREE_VERIFIED ? c->tn + 1 : 0);
+    if (first < 0 || n < 0 || first > held || n > held - first) return fail(c, HIVIS_EINVAL, "rows %d .. %d of %d", first, first + n - 1, held);
+    if (n == 0) return HIVIS_OK;
+    std::vector<int> table(c->kv4_max_blocks), slots(n);
+    HIP_TRY(c, hipMemcpyAsync(table.data(), c->kv4_table + (size_t)seq * c->kv4_max_blocks, table.size() * sizeof(int), hipMemcpyDeviceToHost, c->stream));
+    HIP_TRY(c, hipStreamSynchronize(c->stream));
+    for (int i = 0; i < n; ++i) slots[i] = table[(first + i) / c->kv4_dims.block] * c->kv4_dims.block + (first + i) % c->kv4_dims.block;
+    const size_t width = (size_t)g.n_kv_heads * g.head_dim, count = (size_t)n * width;
+    char* mem = nullptr;
+    HIP_TRY(c, hipMalloc((void**)&mem, 2 * count * sizeof(float) + n * sizeof(int)));
+    float* dk = (float*)mem; float* dv = dk + count; int* ds = (int*)(dv + count);
+    RowsArgs r{};
+    r.d = c->kv4_dims; r.k = dk; r.v = dv; r.row = width; r.head = g.head_dim; r.n = n; r.slots = ds; r.pool = c->kv4_mem + layer * c->kv4_pool;
+    int rc = HIVIS_OK;
+    hipError_t e = hipMemcpyAsync(ds, slots.data(), n * sizeof(int), hipMemcpyHostToDevice, c->stream);
+    if (e == hipSuccess) rc = kv4_read_launch(c->stream, KV4_ROWS_F32, r);
+    if (e == hipSuccess && !rc) e = hipMemcpyAsync(k, dk, count * sizeof(float), hipMemcpyDeviceToHost, c->stream);
+    if (e == hipSuccess && !rc) e = hipMemcpyAsync(v, dv, count * sizeof(float), hipMemcpyDeviceToHost, c->stream);
+    const hipError_t e2 = hipStreamSynchronize(c->stream);
+    (void)hipFree(mem);
+    if (rc) return fail(c, rc, "%s", hivis_last_error(nullptr));
+    if (e != hipSuccess || e2 != hipSuccess) return fail(c, HIVIS_EHIP, "reading the cache back failed: %s", hipGetErrorString(e != hipSuccess ? e : e2));
+    // cached keys have the dims of a rotary pair (i, i + hd / 2) side by side
+    std::vector<float> row(g.head_dim);
+    for (size_t r = 0; r < count; r += g.head_dim) {
+        std::copy(k + r, k + r + g.head_dim, row.begin());
+        for (int i = 0; i < g.head_dim / 2; ++i) { k[r + i] = row[2 * i]; k[r + g.head_dim / 2 + i] = row[2 * i + 1]; }
+    }
+    return HIVIS_OK;
+}
+
 int hivis_kv_lengths(hivis_ctx* c, int32_t* target_len, int32_t* drafter_len) {
     if (!c) return HIVIS_EINVAL;
     const int B = c->cfg.batch;
@@ -2750,7 +2957,8 @@ int hivis_algorithmic_bytes(hivis_ctx* c, double* verify_bytes, double* draft_st
     const double b = c->esize, d = g.d, qd = (double)g.n_q_heads * g.head_dim, kd = (double)g.n_kv_heads * g.head_dim, F = g.ffn, V = g.vocab;
     const double w_layer = (2 * d * qd + 2 * d * kd + 3 * d * F) * b;
     double kv_t = 0, kv_d = 0;
-    for (int s = 0; s < g.batch; ++s) { kv_t += 2.0 * c->h_tlen[s] * kd * b * g.n_layers; kv_d += 2.0 * c->h_dlen[s] * kd * b; }
+    const double kv_row = c->kv4 ? g.n_kv_heads * (g.head_dim + g.head_dim / 16) : 2.0 * kd * b;
+    for (int s = 0; s < g.batch; ++s) { kv_t += c->h_tlen[s] * kv_row * g.n_layers; kv_d += 2.0 * c->h_dlen[s] * kd * b; }
     if (verify_bytes) *verify_bytes = g.n_layers * w_layer + V * d * b + kv_t;
     // (the method's bytes: the fusion FC as [2d x d] weights, also where the library reads only w1 and a table row per sequence)
     if (draft_step_bytes) *draft_step_bytes = w_layer + 2 * d * d * b + V * d * b + kv_d;

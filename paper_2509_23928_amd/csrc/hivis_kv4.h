@@ -6,8 +6,7 @@
 // A block holds block_tokens rows of every key head; per head one run of memory: key codes [T][HD/2] | value codes [T][HD/2] |
 // key scales [T][HD/32] | value scales [T][HD/32].
 #pragma once
-#include <hip/hip_runtime.h>
-#include <stdint.h>
+#include "hivis_kv4_args.h"
 
 namespace hivis {
 
@@ -17,11 +16,6 @@ typedef float kv4_f32x4 __attribute__((ext_vector_type(4)));
 typedef short kv4_s16x4 __attribute__((ext_vector_type(4)));
 typedef unsigned kv4_u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned kv4_u32x2 __attribute__((ext_vector_type(2)));
-
-// What the kernels know of a cache
-struct Kv4Dims { int heads, hd, block, shift, n_blocks; };       // block = 1 << shift rows
-
-__host__ __device__ inline int kv4_chunk(int hd, int block) { return block * (hd + hd / 16); }      // bytes of one head in one block
 
 // Scale byte of a group whose largest magnitude has the bits `a` (sign cleared): the smallest power of two at which no value is cut by more than
 // half a step (a <= 7 scale; the largest code stands for 6 and its step is 2), between 2^-100 (products of two held values stay normal numbers) and
@@ -37,12 +31,6 @@ __host__ __device__ inline int kv4_scale_byte(unsigned a) {
 // timing.  Latency bound: one workgroup, a wavefront for every 64 sequences up to sixteen (and rounds of 1024 beyond), sums in registers, one batch of requests
 // per step; blocks are moved by all threads, a block each.  The slots of many rows are a launch of their own, over the chip (plan_fused).
 constexpr int PLAN_MAX = 1024;                               // threads at most
-
-struct PlanArgs {
-    int n, max_blocks, shift, n_blocks, max_rows;
-    const int *keep, *add; int *held, *table, *free_list, *row_start, *slots, *positions, *status;
-    bool fill;                                               // slots and positions in the same launch
-};
 
 struct PlanShared { long long part[PLAN_MAX / 64]; int from[PLAN_MAX], base[PLAN_MAX], s[PLAN_MAX]; };
 
@@ -88,7 +76,7 @@ __device__ inline void plan_fill(const PlanArgs& a, int r, int total) {
     if (r < total) {
         int lo = 0, hi = a.n - 1;                            // the last sequence that starts at or before r
         while (lo < hi) { const int mid = (lo + hi + 1) >> 1; if (a.row_start[mid] <= r) lo = mid; else hi = mid - 1; }
-        pos = a.keep[lo] + r - a.row_start[lo];
+        pos = (a.keep ? a.keep[lo] : 0) + r - a.row_start[lo];
         slot = (a.table[(size_t)lo * a.max_blocks + (pos >> a.shift)] << a.shift) + (pos & ((1 << a.shift) - 1));
     }
     a.slots[r] = slot;
@@ -103,7 +91,7 @@ __global__ __launch_bounds__(PLAN_MAX) void kv4_plan_kernel(PlanArgs a) {
     if (count < 0 || count > a.n_blocks) count = 0;
     // One round: everything stays in registers.  More: what a sequence asks for is read again for every sum (held changes only where blocks are given back).
     int keep = 0, add = 0, held = 0, need = -1, status = 0;
-    auto load = [&](int s) { keep = add = held = 0; need = -1; if (s < a.n) { keep = a.keep[s]; add = a.add[s]; held = a.held[s]; need = plan_need(a, keep, add, held); } };
+    auto load = [&](int s) { keep = add = held = 0; need = -1; if (s < a.n) { keep = a.keep ? a.keep[s] : 0; add = a.add ? a.add[s] : a.add_each; held = a.held[s]; need = plan_need(a, keep, add, held); } };
     long long rows = 0, total;
     // ---- rows in order: who has room among the slots
     for (int r = 0; r < rounds; ++r) {
@@ -176,12 +164,6 @@ __global__ __launch_bounds__(256) void kv4_plan_slots_kernel(PlanArgs a) {
 // Rows as callers hold them: T (float, __bf16, or Kv4Halves: a high and a low IEEE half per value, all high halves of a row first), row r of head h at
 // r * row + h * head (elements; Kv4Halves: values).
 struct Kv4Halves {};
-struct RowsArgs {
-    Kv4Dims d; const void *k, *v; long long row, head; int n; const int* slots; uint8_t* pool;
-    // rows of several sequences at equal distance instead (slots from the plan all the same): row r is row first[s] + r % m of sequence r / m, sequences `seq` elements apart
-    const int* first; int m, offset; long long seq;
-};
-
 template <typename T> __device__ inline void kv4_load8(const T* p, float (&x)[8]);
 template <> __device__ inline void kv4_load8<float>(const float* p, float (&x)[8]) {
     const float4 a = *(const float4*)p, b = *(const float4*)(p + 4);
@@ -305,18 +287,25 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(RowsArgs a) {
     }
 }
 
-// ---- attention ------------------------------------------------------------------------------------------------------------------------------
-struct Kv4AttnArgs {
-    Kv4Dims d; int group, n_seqs, n_rows, max_rows, max_blocks, tiles; // group: query heads per key head; tiles: row tiles per sequence in the grid
-    float scale2;                                            // |softmax scale| times log2 e; negative ones negate the queries
-    bool negate;
-    const uint8_t* pool; const int *table, *row_start, *kv_len;
-    const void* q; long long ldq; const unsigned long long* mask; void* out; long long ldo;
-    // rows of the context's passes instead of row_start: m rows of every sequence, row r of sequence s at s * qrows + r in q and s * m + r in out, lengths kv_len[seq0 + s] + len_add
-    int m, qrows, seq0, len_add;
-    float* ws; int* cnt;                                     // kv4_stream_kernel: partials, arrivals per item (zero between launches)
-};
+// Rows of sequence 0 from positions len + path[j] to len + j, j = 1 .. *n, in the pools of all layers (blockIdx.x) for each key head (blockIdx.y): all are read before any is
+// written, for one row's place can be another's origin.
+__global__ __launch_bounds__(256) void kv4_move_kernel(Kv4Dims d, uint8_t* mem, long long pool, const int* table, const int* len, const int* n, const int* path) {
+    extern __shared__ uint16_t kv4_moved[];                  // [row][codes of the key, of the value, their scales], two bytes each
+    const int units = (d.hd + d.hd / 16) / 2, rows = n[0];
+    uint8_t* const base = mem + blockIdx.x * pool;
+    auto at = [&](int pos, int u) -> uint16_t* {
+        uint8_t* c = base + ((size_t)table[pos >> d.shift] * d.heads + blockIdx.y) * kv4_chunk(d.hd, d.block);
+        const int r = pos & (d.block - 1), code = d.hd / 4, scale = d.hd / 64;
+        if (u < 2 * code) return (uint16_t*)(c + ((u >= code) * d.block + r) * (d.hd / 2)) + u % code;
+        u -= 2 * code;
+        return (uint16_t*)(c + d.block * d.hd + ((u >= scale) * d.block + r) * (d.hd / 32)) + u % scale;
+    };
+    for (int i = threadIdx.x; i < rows * units; i += 256) kv4_moved[i] = *at(len[0] + path[1 + i / units], i % units);
+    __syncthreads();
+    for (int i = threadIdx.x; i < rows * units; i += 256) *at(len[0] + 1 + i / units, i % units) = kv4_moved[i];
+}
 
+// ---- attention ------------------------------------------------------------------------------------------------------------------------------
 // Both kernels multiply alike.  A tile of 16 (row, query head) pairs of one key head, row by row, is the N dimension of
 //   S^T[key][pair] = K Q^T          mfma 16x16x32, 16 keys as rows
 //   O^T[dim][pair] += V^T P^T       a lane's weights of keys 4g .. 4g+3 of two 16-key halves are its operand as they come out of S^T (contractions take any
@@ -767,13 +756,14 @@ __global__ __launch_bounds__(256, (kv4_stream_per_cu<T, HD>())) void kv4_stream_
     const Item x = due_it[w];
     const Kv4Seq s = x.s;
     const int h = x.h, p0 = x.ti * 16 * RT, count = min(16 * RT, s.pairs - p0);
-    const int w0 = kv4_div(x.begins, per), parts = kv4_div(x.begins + x.nb - 1, per) - w0 + 1, item = (x.seq * a.tiles + x.ti) * a.d.heads + h;
-    if (tid == 0) last = __hip_atomic_fetch_add(&a.cnt[item], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == parts - 1;
+    // (counted where the item begins: one at most begins in a run and goes on behind it)
+    const int w0 = kv4_div(x.begins, per), parts = kv4_div(x.begins + x.nb - 1, per) - w0 + 1;
+    if (tid == 0) last = __hip_atomic_fetch_add(&a.cnt[w0], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == parts - 1;
     __syncthreads();
     const bool mine = last;
     __syncthreads();
     if (!mine) continue;
-    if (tid == 0) __hip_atomic_store(&a.cnt[item], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (tid == 0) __hip_atomic_store(&a.cnt[w0], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     // Merge, in the order of the keys (the same whoever merges): a thread takes four dims of a pair and eight partials at a time, all requested at once with their
     // refs and denominators; where there are fewer pairs than threads for them, several threads share the partials and add up in LDS.
     int sh_pr = 0;                                           // pairs padded to a power of two

@@ -10,22 +10,14 @@
 // than the pass: 128 rows of 152064, top 20, 41 us, and 51 with a barrier per chunk.)  Where too many are equal to the bound (a row that is mostly one value):
 // k rounds of maxima, each thread with its own next one.  The workgroup that finishes a row's last segment merges.
 #pragma once
-#include <hip/hip_runtime.h>
-#include <stdint.h>
+#include "hivis_logprobs_args.h"
 
 namespace hivis {
 
-constexpr int LOGPROBS_MAX_TOP = 32, LOGPROBS_NT = 256, LOGPROBS_PER = 16, LOGPROBS_CHUNK = LOGPROBS_NT * LOGPROBS_PER, LOGPROBS_WGS = 1024;
+constexpr int LOGPROBS_NT = 256, LOGPROBS_PER = 16, LOGPROBS_CHUNK = LOGPROBS_NT * LOGPROBS_PER, LOGPROBS_WGS = 1024;
 constexpr int LOGPROBS_LIST = 512;                           // keys ranked together, at most
 constexpr int LOGPROBS_AHEAD = 4;                            // keys of the segments that a thread of the merging workgroup takes at a time
 constexpr int LOGPROBS_STATS = 4;                            // words of a segment's partial before its keys: maximum, z, s, whether it has a NaN
-
-struct LogprobsArgs {
-    const void* x; long long ld; int rows, vocab; float inv_temp;
-    const int* tokens; int n_tokens; float *logprob, *entropy;
-    int top; int* top_ids; float* top_logprobs;
-    int chunks, segs; int* cnt; uint32_t* part;              // chunks of a segment; segments of a row, arrivals per row (zero between launches), partials [row][seg][STATS + 2 top]
-};
 
 // order of the alternatives as one number: larger logits first, then lower ids; 0 is below all
 typedef unsigned long long lp_key;

@@ -148,14 +148,15 @@ static Kv4Plan kv4_plan_attend(const Kv4Dims& d, bool f32, int group, int n_seqs
     }
     return p;
 }
-static long long kv4_counters(const Kv4Plan& p) { return (p.items * 4 + 255) / 256 * 256; }
-static long long kv4_space(const Kv4Plan& p, int hd) { return p.rows ? 16 : kv4_counters(p) + 2LL * p.wgs * 16 * (hd + 2) * 4; }
+// A workspace: counters, of the same number in every call (what one call leaves there is zero for the next, of whatever size), then partials
+constexpr int WS_COUNTERS = 1024 * sizeof(int);
+static long long kv4_space(const Kv4Plan& p, int hd) { return p.rows ? 16 : WS_COUNTERS + 2LL * p.wgs * 16 * (hd + 2) * 4; }
 
 int kv4_attend_launch(hipStream_t st, int dtype, Kv4AttnArgs a, int max_rows, int max_len, void* ws) {
     const bool f32 = dtype == HIVIS_F32;
     const Kv4Plan p = kv4_plan_attend(a.d, f32, a.group, a.n_seqs, max_rows, max_len);
     const long long sh = ((long long)a.n_seqs * a.d.heads + 7) / 8 * 8;
-    a.tiles = p.tiles; a.max_rows = max_rows; a.cnt = (int*)ws; a.ws = (float*)((char*)ws + kv4_counters(p));
+    a.tiles = p.tiles; a.max_rows = max_rows; a.cnt = (int*)ws; a.ws = (float*)((char*)ws + WS_COUNTERS);
 #define KV4_ROWS_(T_, HD_, RT_)                                                                                                                               \
     do {                                                                                                                                                      \
         constexpr int lds_ = 2 * 64 * (kv4_vstride<HD_>() + kv4_kstride<HD_>()) + 3 * (3 + HD_ / 32) * 8;                                                     \
@@ -184,12 +185,21 @@ static void logprobs_cut(int rows, int vocab, int* chunks, int* segs) {
     *chunks = (all + want - 1) / want;
     *segs = (all + *chunks - 1) / *chunks;
 }
-static long long logprobs_counters(int rows) { return ((long long)rows * 4 + 255) / 256 * 256; }
+static_assert(LOGPROBS_WGS / 2 <= WS_COUNTERS / (int)sizeof(int), "rows in more than one segment");
 
+long long kv4_stream_space(int hd) { return WS_COUNTERS + 2LL * 1024 * 16 * (hd + 2) * 4; }
+
+int kv4_move_launch(hipStream_t st, const Kv4Dims& d, uint8_t* mem, long long pool, int layers, const int* table, const int* len, const int* n, const int* path, int depth) {
+    hipLaunchKernelGGL(kv4_move_kernel, dim3(layers, d.heads), dim3(256), depth * (d.hd + d.hd / 16), st, d, mem, pool, table, len, n, path);
+    OP_TRY(hipGetLastError());
+    return HIVIS_OK;
+}
+
+// ---- log probabilities ----
 int logprobs_launch(hipStream_t st, int dtype, LogprobsArgs a, void* ws) {
     if (a.rows == 0) return HIVIS_OK;
     logprobs_cut(a.rows, a.vocab, &a.chunks, &a.segs);
-    a.cnt = (int*)ws; a.part = (uint32_t*)((char*)ws + logprobs_counters(a.rows));
+    a.cnt = (int*)ws; a.part = (uint32_t*)((char*)ws + WS_COUNTERS);
 #define LOGPROBS_(T_, TOP_) hipLaunchKernelGGL((logprobs_kernel<T_, TOP_>), dim3(a.segs, a.rows), dim3(LOGPROBS_NT), 0, st, a)
     if (dtype == HIVIS_F32) { if (a.top) LOGPROBS_(float, true); else LOGPROBS_(float, false); }
     else { if (a.top) LOGPROBS_(__bf16, true); else LOGPROBS_(__bf16, false); }
@@ -201,7 +211,7 @@ int logprobs_launch(hipStream_t st, int dtype, LogprobsArgs a, void* ws) {
 long long logprobs_space(int rows, int vocab, int top) {
     int chunks, segs;
     logprobs_cut(rows, vocab, &chunks, &segs);
-    return logprobs_counters(rows) + (segs > 1 ? (long long)rows * segs * (LOGPROBS_STATS + 2 * top) * 4 : 0) + 16;
+    return segs > 1 ? WS_COUNTERS + (long long)rows * segs * (LOGPROBS_STATS + 2 * top) * 4 : 16;
 }
 
 }  // namespace hivis
@@ -225,7 +235,7 @@ int hivis_kv4_plan(void* hip_stream, int32_t n_seqs, int32_t max_blocks, int32_t
     CHECK(keep && add && held && table && free_list && row_start && status && (slots || max_rows == 0), "null argument");
     if (int rc = check_devices({{keep, "keep"}, {add, "add"}, {held, "held"}, {table, "table"}, {free_list, "free_list"}, {row_start, "row_start"}, {slots, "slots"},
                                 {positions, "positions"}, {status, "status"}})) return rc;
-    return kv4_plan_launch((hipStream_t)hip_stream, PlanArgs{n_seqs, max_blocks, d.shift, n_blocks, max_rows, keep, add, held, table, free_list, row_start, slots, positions, status, false});
+    return kv4_plan_launch((hipStream_t)hip_stream, PlanArgs{n_seqs, max_blocks, d.shift, n_blocks, max_rows, keep, add, held, table, free_list, row_start, slots, positions, status, 0, false});
 }
 
 int hivis_kv4_append(void* hip_stream, const hivis_kv4_shape* shape, int32_t dtype, const void* k, const void* v, int64_t row_stride, int64_t head_stride, int32_t n_rows,
