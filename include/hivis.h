@@ -286,7 +286,8 @@ int64_t hivis_kv4_pool_bytes(const hivis_kv4_shape *shape);
  *   and keeps what it held.
  * Blocks are given back first, the last sequence's last block first, and then taken in order of the sequences: the same
  * lengths give the same tables, and blocks taken by a call and given back by the next leave the list as it was.  Sequence s
- * is refused (1, 3) exactly if the sequences up to and with s need more than there is.
+ * is refused for blocks (1) exactly if it needs some and the sequences up to and with it need more than there are, for rows
+ * (3) exactly if the sequences up to and with it have more than max_rows (one that adds none among them).
  * Errors: EINVAL, EHIP. */
 int hivis_kv4_plan(void *hip_stream, int32_t n_seqs, int32_t max_blocks, int32_t block_tokens, int32_t n_blocks, const int32_t *keep, const int32_t *add, int32_t *held,
                    int32_t *table, int32_t *free_list, int32_t *row_start, int32_t *slots, int32_t *positions, int32_t max_rows, int32_t *status);

@@ -314,7 +314,7 @@ __global__ __launch_bounds__(256) void kv4_move_kernel(Kv4Dims d, uint8_t* mem, 
 // weights are rounded to bf16 (off by at most 2^-8 each, as the result is).
 // Weights are 2^(s - ref); ref follows a pair's largest score s only when that outgrows it by 2^8, so most tiles need no maximum over lanes and no
 // rescaling; sums and maxima are fp32.
-constexpr float KV4_REF0 = -1.0e30f;                         // ref before the first key (finite: a difference of two infinities would be no number)
+constexpr float KV4_REF0 = -3.0e38f;                         // ref before the first key (finite: a difference of two infinities would be no number)
 constexpr float KV4_SLACK = 8.f;
 constexpr int KV4_UNIT = 128;                                // keys of a unit of work: four wavefronts, 32 each
 constexpr int KV4_ITEM_COST = 2;                             // what opening and closing an item costs, in units
