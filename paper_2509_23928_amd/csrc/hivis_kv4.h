@@ -13,6 +13,7 @@ namespace hivis {
 typedef __bf16 kv4_bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 kv4_bf16x8 __attribute__((ext_vector_type(8)));
 typedef float kv4_f32x4 __attribute__((ext_vector_type(4)));
+typedef float kv4_f32x16 __attribute__((ext_vector_type(16)));
 typedef short kv4_s16x4 __attribute__((ext_vector_type(4)));
 typedef unsigned kv4_u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned kv4_u32x2 __attribute__((ext_vector_type(2)));
@@ -321,6 +322,7 @@ constexpr int KV4_ITEM_COST = 2;                             // what opening and
 
 // LDS rows: the transposing read of four rows, and eight lanes' 16-byte accesses, meet all banks
 template <int HD> constexpr int kv4_vstride() { return HD * 2 + 32; }
+template <int HD> constexpr int kv4_vstride32() { return HD * 2 + 64; }
 template <int HD> constexpr int kv4_kstride() { return HD * 2 + 16; }
 
 __device__ inline float kv4_xmax(float x) {                  // over the four lanes that share a pair
@@ -410,56 +412,59 @@ __device__ inline void kv4_queries(const Kv4AttnArgs& a, const Kv4Seq& s, int h,
         for (int j = 0; j < HD / 32; ++j) raw[t][j] = *(const Kv4Raw<T>*)(q + dim(g, j));
     }
 }
+template <typename T, int NP>
+__device__ inline void kv4_query_part(bool negate, const Kv4Raw<T>& raw, kv4_bf16x8 (&f)[NP]) {
+    if constexpr (sizeof(T) == 2) {
+        kv4_u32x4 x = raw.x[0];
+        if (negate) x ^= 0x80008000u;
+        f[0] = __builtin_bit_cast(kv4_bf16x8, x);
+    } else {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { x[e] = __uint_as_float(raw.x[e >> 2][e & 3]); if (negate) x[e] = -x[e]; }
+        kv4_parts<NP>(x, f);
+    }
+}
 template <typename T, int HD, int RT, int NP>
 __device__ inline void kv4_query_parts(const Kv4AttnArgs& a, const Kv4Raw<T> (&raw)[RT][HD / 32], kv4_bf16x8 (&qf)[RT][HD / 32][NP]) {
 #pragma unroll
     for (int t = 0; t < RT; ++t)
 #pragma unroll
-        for (int j = 0; j < HD / 32; ++j) {
-            if constexpr (sizeof(T) == 2) {
-                kv4_u32x4 x = raw[t][j].x[0];
-                if (a.negate) x ^= 0x80008000u;
-                qf[t][j][0] = __builtin_bit_cast(kv4_bf16x8, x);
-            } else {
-                float x[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) { x[e] = __uint_as_float(raw[t][j].x[e >> 2][e & 3]); if (a.negate) x[e] = -x[e]; }
-                kv4_parts<NP>(x, qf[t][j]);
-            }
-        }
+        for (int j = 0; j < HD / 32; ++j) kv4_query_part<T, NP>(a.negate, raw[t][j], qf[t][j]);
 }
 
-// One tile of pairs against NH halves of 16 keys: scores x to weights in operand parts; o, ref and l follow.  vis: the keys that the lane's pair sees (bit 16 c + 4 g + r:
-// x[c][r]), unless all do (plain).
-template <int NB, int NH, int NP>
-__device__ inline void kv4_softmax(kv4_f32x4 (&x)[NH], float scale2, bool plain, unsigned long long vis, int g, kv4_f32x4 (&o)[NB], float& ref, float& l, kv4_bf16x8 (&pf)[NH / 2][NP]) {
-    float p[4 * NH];
-    unsigned on[2] = {0, 0};
-    if (!plain) {
-        vis >>= 4 * g;
-        on[0] = (unsigned)vis; on[1] = (unsigned)(vis >> 32);
+// One tile of pairs against NH halves of 16 keys, scores x (bit 16 c + 4 g + r of a lane's word: x[c][r]).
+// The keys that a pair does not see weigh nothing (a scale of zero is a tiny one in scale2, so that no product of zero and infinity comes up).
+template <int NH>
+__device__ inline void kv4_hide(kv4_f32x4 (&x)[NH], unsigned long long vis, int g) {
+    vis >>= 4 * g;
+    const unsigned on[2] = {(unsigned)vis, (unsigned)(vis >> 32)};
 #pragma unroll
-        for (int i = 0; i < 4 * NH; ++i)                     // (an all-ones or all-zeros word selects)
-            x[i >> 2][i & 3] = ((int)(on[i >> 3] << (31 - 16 * (i >> 2 & 1) - (i & 3))) >> 31) ? x[i >> 2][i & 3] : -INFINITY;
-    }
+    for (int i = 0; i < 4 * NH; ++i)                         // (an all-ones or all-zeros word selects)
+        x[i >> 2][i & 3] = ((int)(on[i >> 3] << (31 - 16 * (i >> 2 & 1) - (i & 3))) >> 31) ? x[i >> 2][i & 3] : -INFINITY;
+}
+template <int NH>
+__device__ inline float kv4_top(const kv4_f32x4 (&x)[NH]) {
     float mx = x[0][0];
 #pragma unroll
     for (int i = 1; i < 4 * NH; ++i) mx = fmaxf(mx, x[i >> 2][i & 3]);
-    mx = mx > -INFINITY ? mx * scale2 : -INFINITY;           // (a scale of zero)
-    if (__any(mx > ref + KV4_SLACK)) {
-        const float to = fmaxf(ref, kv4_xmax(mx)), f = __builtin_amdgcn_exp2f(ref - to);
-        ref = to;
-        l *= f;
+    return mx;
+}
+// ref follows a largest score of mx; what was added up so far follows it
+template <int NB>
+__device__ inline void kv4_follow(float mx, kv4_f32x4 (&o)[NB], float& ref, float& l) {
+    const float to = fmaxf(ref, kv4_xmax(mx)), f = __builtin_amdgcn_exp2f(ref - to);
+    ref = to;
+    l *= f;
 #pragma unroll
-        for (int t = 0; t < NB; ++t) o[t] *= f;
-    }
+    for (int t = 0; t < NB; ++t) o[t] *= f;
+}
+// scores to weights in operand parts, and their sum
+template <int NH, int NP>
+__device__ inline void kv4_weights(const kv4_f32x4 (&x)[NH], float scale2, float ref, float& l, kv4_bf16x8 (&pf)[NH / 2][NP]) {
+    float p[4 * NH], s[4];
 #pragma unroll
     for (int i = 0; i < 4 * NH; ++i) p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i >> 2][i & 3], scale2, -ref));
-    if (!plain) {
-#pragma unroll
-        for (int i = 0; i < 4 * NH; ++i) p[i] = ((int)(on[i >> 3] << (31 - 16 * (i >> 2 & 1) - (i & 3))) >> 31) ? p[i] : 0.f;
-    }
-    float s[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) { s[i] = p[i] + p[i + 4]; if (NH == 4) s[i] += p[(i + 8) % (4 * NH)] + p[(i + 12) % (4 * NH)]; }
     l += (s[0] + s[1]) + (s[2] + s[3]);
@@ -692,7 +697,12 @@ __global__ __launch_bounds__(256, (kv4_stream_per_cu<T, HD>())) void kv4_stream_
         }
         kv4_bf16x8 pf[RT][1][NP];
 #pragma unroll
-        for (int r = 0; r < RT; ++r) kv4_softmax<NB, 2, NP>(x[r], a.scale2, plain, plain ? 0 : see[r].of(k0) & held, g, o[r], ref[r], l[r], pf[r]);
+        for (int r = 0; r < RT; ++r) {
+            if (!plain) kv4_hide(x[r], see[r].of(k0) & held, g);
+            const float mx = kv4_top(x[r]) * a.scale2;
+            if (__any(mx > ref[r] + KV4_SLACK)) kv4_follow(mx, o[r], ref[r], l[r]);
+            kv4_weights<2, NP>(x[r], a.scale2, ref[r], l[r], pf[r]);
+        }
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
             const kv4_bf16x8 vf = kv4_vfrag<HD>(vt, b, lane);
@@ -814,25 +824,26 @@ __global__ __launch_bounds__(256, (kv4_stream_per_cu<T, HD>())) void kv4_stream_
 }
 
 // ---- many rows (prompts): bound by the matrix cores and the vector work of the softmax ----
-// A workgroup is one key head of one sequence and 64 RT pairs, 16 RT per wavefront; the cache is expanded to bf16 once per workgroup, 64 keys at a time, into two
+// A workgroup is one key head of one sequence and 64 pairs, 16 per wavefront; the cache is expanded to bf16 once per workgroup, 64 keys at a time, into two
 // LDS buffers in turn (one barrier per tile).  A thread expands a quarter of one key and of one value: one wide load and one scale each, requested
 // a tile ahead.
-template <typename T, int HD, int RT>
+template <typename T, int HD>
 __global__ __launch_bounds__(256, 2) void kv4_rows_kernel(Kv4AttnArgs a) {
-    constexpr int NP = sizeof(T) == 4 ? 3 : 1, STEPS = HD / 32, NB = HD / 16, KT = 64, VSTRIDE = kv4_vstride<HD>(), KSTRIDE = kv4_kstride<HD>();
+    constexpr int RT = 1, NP = sizeof(T) == 4 ? 3 : 1, STEPS = HD / 32, NB = HD / 16, KT = 64, VSTRIDE = kv4_vstride<HD>(), KSTRIDE = kv4_kstride<HD>();
     constexpr int BUF = KT * (VSTRIDE + KSTRIDE), NG = HD / 32;
     extern __shared__ __align__(16) char kv4_lds[];
     // Bits of a tile's keys: [0] any of the others; [1] not held; [2] the key's scale says NaN; [3 ..] those of the values' groups.  Three tiles in turn: written
     // before a tile's barrier, read behind it, cleared behind the next one.
     unsigned long long (*const odd)[3 + NG] = (unsigned long long (*)[3 + NG])(kv4_lds + 2 * BUF);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g = lane >> 4;
-    // (the longest first; sequences in turn, or each would always meet the same shader engine of a chiplet: four prompts of 641 to 3008 rows 405 us)
-    const int sh = blockIdx.x, ti = a.tiles - 1 - blockIdx.y;
+    // The last rows of every sequence, which see most, first (by row tile alone, what starts last may be long: four prompts of 641 to 3008 rows 199 us instead of 175);
+    // sequences in turn, or each would always meet the same shader engine of a chiplet (405 us)
+    const int sh = blockIdx.x;
     if (sh >= a.n_seqs * a.d.heads) return;
     const int h = sh % a.d.heads, seq = (int)((sh / a.d.heads + blockIdx.y) % a.n_seqs);
     const Kv4Seq s = kv4_seq(a, seq);
-    const int pairs = s.pairs, p0 = ti * 64 * RT, w0 = p0 + wave * 16 * RT;
-    if (p0 >= pairs) return;
+    const int pairs = s.pairs, ti = (pairs + 64 * RT - 1) / (64 * RT) - 1 - (int)blockIdx.y, p0 = ti * 64 * RT, w0 = p0 + wave * 16 * RT;
+    if (ti < 0) return;
     const int limit = a.mask ? s.len : s.len - s.rows + min(p0 + 64 * RT - 1, pairs - 1) / a.group + 1;
     const int mine = w0 >= pairs ? 0 : a.mask ? s.len : s.len - s.rows + min(w0 + 16 * RT - 1, pairs - 1) / a.group + 1;       // of this wavefront
     const int all = s.len - s.rows + (a.mask ? 0 : w0 / a.group + 1);
@@ -924,7 +935,12 @@ __global__ __launch_bounds__(256, 2) void kv4_rows_kernel(Kv4AttnArgs a) {
         }
         kv4_bf16x8 pf[RT][2][NP];
 #pragma unroll
-        for (int r = 0; r < RT; ++r) kv4_softmax<NB, 4, NP>(x[r], a.scale2, plain, plain ? 0 : see[r].of(k0) & ~gone, g, o[r], ref[r], l[r], pf[r]);
+        for (int r = 0; r < RT; ++r) {
+            if (!plain) kv4_hide(x[r], see[r].of(k0) & ~gone, g);
+            const float mx = kv4_top(x[r]) * a.scale2;
+            if (__any(mx > ref[r] + KV4_SLACK)) kv4_follow(mx, o[r], ref[r], l[r]);
+            kv4_weights<4, NP>(x[r], a.scale2, ref[r], l[r], pf[r]);
+        }
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -946,6 +962,187 @@ __global__ __launch_bounds__(256, 2) void kv4_rows_kernel(Kv4AttnArgs a) {
             for (int b = 0; b < NB; ++b)
                 kv4_store4<T, HD>(a, s, h, pr, 16 * b + 4 * g, o[r][b] * inv);
         }
+    }
+}
+
+// ---- more rows than fill the chip ----
+// As above with products of 32 x 32: 32 pairs per wavefront, 128 per workgroup, for half the reads of LDS per product.  Half as many instructions of the matrix cores leave
+// more room for vector work beside them (per SIMD, 128 multiply-adds beside the products of two wavefronts: 842 cycles with 16 x 16, 723 with 32 x 32).  Four
+// prompts of 641 to 3008 rows, 32 heads: 163 us, 0.81 PFLOP/s (tiles of 16 x 16, two per wavefront: 175; scores a tile ahead of the weights 173; two workgroups' work
+// in one, keys shared: 223; 32 keys per tile and three wavefronts per SIMD: 177; 64 pairs per wavefront: registers spill).
+// A lane has one pair and, of every eight keys, the four of its half.  Keys of KS at a time go through the softmax (32 where the operand parts of 64 would not
+// fit the registers).
+template <typename T, int HD>
+__global__ __launch_bounds__(256, 2) void kv4_rows32_kernel(Kv4AttnArgs a) {
+    constexpr int NP = sizeof(T) == 4 ? 3 : 1, KS = sizeof(T) == 4 ? 32 : 64, STEPS = HD / 16, NB = HD / 32, KT = 64, VSTRIDE = kv4_vstride32<HD>(), KSTRIDE = kv4_kstride<HD>();
+    constexpr int BUF = KT * (VSTRIDE + KSTRIDE), NG = HD / 32, NC = HD / 32;
+    extern __shared__ __align__(16) char kv4_lds[];
+    // Bits of a tile's keys: [0] any of the next two; [1] not held; [2] the key's scale says NaN; [3] any of the others; [4 ..] the scale of a value's group does.
+    // Three tiles in turn: written before a tile's barrier, read behind it, cleared behind the next one.
+    unsigned long long (*const odd)[4 + NG] = (unsigned long long (*)[4 + NG])(kv4_lds + 2 * BUF);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n32 = lane & 31, hh = lane >> 5;
+    const int sh = blockIdx.x;
+    if (sh >= a.n_seqs * a.d.heads) return;
+    const int h = sh % a.d.heads, seq = (int)((sh / a.d.heads + blockIdx.y) % a.n_seqs);
+    const Kv4Seq s = kv4_seq(a, seq);
+    const int pairs = s.pairs, ti = (pairs + 127) / 128 - 1 - (int)blockIdx.y, p0 = ti * 128, w0 = p0 + wave * 32;
+    if (ti < 0) return;
+    const int limit = a.mask ? s.len : s.len - s.rows + min(p0 + 127, pairs - 1) / a.group + 1;
+    const int mine = w0 >= pairs ? 0 : a.mask ? s.len : s.len - s.rows + min(w0 + 31, pairs - 1) / a.group + 1;       // of this wavefront
+    const int all = s.len - s.rows + (a.mask ? 0 : w0 / a.group + 1);
+    const int* row = a.table + (size_t)(a.row_start ? seq : a.seq0 + seq) * a.max_blocks;
+    const int bytes = kv4_chunk(HD, a.d.block);
+    if (threadIdx.x < 3 * (4 + NG)) ((unsigned long long*)odd)[threadIdx.x] = 0;
+    __syncthreads();
+
+    // a wavefront's 16 keys lie in one block: the address is the same for all lanes but for an offset
+    const int kr = threadIdx.x >> 2, kq = threadIdx.x & 3;   // this thread's key of a tile and quarter
+    const unsigned at_code = (lane >> 2) * (HD / 2) + kq * (HD / 8), at_scale = (lane >> 2) * (HD / 32) + kq * (HD / 4) / 32;
+    struct Part { unsigned c[NC], b; } kp, vp;               // a quarter of a key and of a value: codes, scale
+    bool in;
+    auto entry = [&](int k0) { const int key = k0 + 16 * wave; return key < s.len ? kv4_scalar(row[key >> a.d.shift]) : -1; };
+    int next = entry(0);                                     // block of the tile that is fetched next, a tile ahead of it
+    auto get = [&](Part& t, const uint8_t* c, int r) {
+        const uint8_t* p = c + r * (HD / 2) + at_code;
+        if constexpr (HD == 128) { const uint4 x = *(const uint4*)p; t.c[0] = x.x; t.c[1] = x.y; t.c[2] = x.z; t.c[3] = x.w; }
+        else { const uint2 x = *(const uint2*)p; t.c[0] = x.x; t.c[1] = x.y; }
+        t.b = (c + a.d.block * HD + r * (HD / 32))[at_scale];
+    };
+    auto fetch = [&](int k0) {
+        const int e = next, r = (k0 + 16 * wave) & (a.d.block - 1);
+        next = entry(k0 + KT);
+        in = e >= 0 && e < a.d.n_blocks;
+        const uint8_t* c = a.pool + ((size_t)(in ? e : 0) * a.d.heads + h) * bytes;
+        get(kp, c, r);
+        get(vp, c, a.d.block + r);
+    };
+    // Values lie in LDS in pieces of eight dims, of every four pieces in an order of the key's: rows 16 banks apart, so neither writes nor reads of four keys meet
+    int to_v[NC];
+#pragma unroll
+    for (int j = 0; j < NC; ++j) to_v[j] = kr * VSTRIDE + (((kq * NC + j) ^ (kr & 3)) * 16);
+    const int from_v = (4 * hh + (lane & 15) / 4) * VSTRIDE + (((lane >> 4 & 1) * 2 + (lane & 3) / 2) ^ ((lane & 15) / 4)) * 16 + (lane & 1) * 8;
+    fetch(0);
+    kv4_bf16x8 qf[STEPS][NP];
+    Kv4Sight see;
+    {
+        const int pair = min(w0 + n32, pairs - 1), i = a.group == 1 ? pair : pair / a.group, hq = h * a.group + pair - i * a.group;
+        see.below = s.len - s.rows + (a.mask ? 0 : i + 1);
+        see.bits = a.mask ? a.mask[s.o0 + i] : 0;
+        const T* q = (const T*)a.q + (long long)(s.q0 + i) * a.ldq + (long long)hq * HD + 8 * hh;
+        Kv4Raw<T> raw[1][STEPS];
+#pragma unroll
+        for (int j = 0; j < STEPS; ++j) raw[0][j] = *(const Kv4Raw<T>*)(q + 16 * j);
+#pragma unroll
+        for (int j = 0; j < STEPS; ++j) kv4_query_part<T, NP>(a.negate, raw[0][j], qf[j]);
+    }
+    kv4_f32x16 o[NB];
+    float ref = KV4_REF0, l = 0.f;
+    unsigned no_number = 0;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[b][i] = 0.f;
+    auto noted = [&](unsigned long long w, unsigned dims, int k0) {
+        for (; w; w &= w - 1) if (see.of(k0 + __builtin_ctzll(w)) & 1) no_number |= dims;
+    };
+    int buf = 0, turn = 0;
+    for (int k0 = 0; k0 < limit; k0 += KT, buf ^= BUF, turn = turn == 2 ? 0 : turn + 1) {
+        unsigned long long* const w = odd[turn];
+        char* const kt = kv4_lds + buf; char* const vt = kt + KT * KSTRIDE;
+        {                                                    // rows that are not held and scales that say NaN stay out of the products
+            const bool held = in && k0 + kr < s.len;
+            if (!held || kp.b == 255 || vp.b == 255) {
+                const unsigned long long bit = 1ull << kr;
+                if (!held || kp.b == 255) { atomicOr(&w[0], bit); atomicOr(&w[held ? 2 : 1], bit); }
+                if (held && vp.b == 255) { atomicOr(&w[3], bit); atomicOr(&w[4 + kq * (HD / 4) / 32], bit); }
+            }
+            const float ks = __uint_as_float((held && kp.b != 255 ? kp.b : 127u) << 23), vs = __uint_as_float((held && vp.b != 255 ? vp.b : 127u) << 23);
+#pragma unroll
+            for (int j = 0; j < NC; ++j) {
+                *(kv4_bf16x8*)(kt + kr * KSTRIDE + (kq * NC + j) * 16) = kv4_expand(kp.c[j], ks);
+                *(kv4_bf16x8*)(vt + to_v[j]) = kv4_expand(vp.c[j], vs);
+            }
+        }
+        __syncthreads();
+        if (k0 + KT < limit) fetch(k0 + KT);
+        if (threadIdx.x < 4 + NG) odd[turn == 0 ? 2 : turn - 1][threadIdx.x] = 0;
+        if (k0 >= mine) continue;
+        const bool any = w[0] != 0;
+        unsigned long long gone = 0;
+        if (any) { gone = w[1]; noted(w[2], 15u, k0); }
+        if (w[3] != 0)
+            for (int b = 0; b < NG; ++b) noted(w[4 + b], 1u << b, k0);
+        const bool plain = k0 + KT <= all && !any;
+        const unsigned long long vis = plain ? 0 : (see.of(k0) & ~gone) >> 4 * hh;
+#pragma unroll
+        for (int part = 0; part < KT / KS; ++part) {
+            kv4_f32x16 x[KS / 32];
+#pragma unroll
+            for (int c = 0; c < KS / 32; ++c) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[c][i] = 0.f;
+#pragma unroll
+                for (int j = 0; j < STEPS; ++j) {
+                    const kv4_bf16x8 kf = *(const kv4_bf16x8*)(kt + (part * KS + 32 * c + n32) * KSTRIDE + (16 * j + 8 * hh) * 2);
+#pragma unroll
+                    for (int p = NP - 1; p >= 0; --p) x[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[j][p], x[c], 0, 0, 0);
+                }
+            }
+            if (!plain)
+#pragma unroll
+                for (int c = 0; c < KS / 32; ++c) {
+                    const unsigned on = (unsigned)(vis >> (part * KS + 32 * c));
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[c][i] = ((int)(on << (31 - 8 * (i / 4) - (i & 3))) >> 31) ? x[c][i] : -INFINITY;
+                }
+            float mx = x[0][0];
+#pragma unroll
+            for (int i = 1; i < KS / 2; ++i) mx = fmaxf(mx, x[i / 16][i & 15]);
+            mx *= a.scale2;
+            if (__any(mx > ref + KV4_SLACK)) {
+                const auto other = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+                const float up = fmaxf(ref, fmaxf(__uint_as_float(other[0]), __uint_as_float(other[1]))), f = __builtin_amdgcn_exp2f(ref - up);
+                ref = up;
+                l *= f;
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[b][i] *= f;
+            }
+            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+            kv4_bf16x8 pf[KS / 16][NP];
+#pragma unroll
+            for (int k = 0; k < KS / 16; ++k) {
+                float e[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) { e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[k / 2][8 * (k & 1) + i], a.scale2, -ref)); sum[i & 3] += e[i]; }
+                kv4_parts<NP>(e, pf[k]);
+            }
+            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+#pragma unroll
+            for (int k = 0; k < KS / 16; ++k)
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    typedef __attribute__((address_space(3))) kv4_s16x4* lds_p;
+                    const char* src = vt + from_v + (part * KS + 16 * k) * VSTRIDE + 64 * b;
+                    union { kv4_s16x4 s[2]; kv4_bf16x8 f; } v;
+                    v.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_p)src);
+                    v.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_p)(src + 8 * VSTRIDE));
+#pragma unroll
+                    for (int p = NP - 1; p >= 0; --p) o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v.f, pf[k][p], o[b], 0, 0, 0);
+                }
+        }
+    }
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+    const float den = __uint_as_float(both[0]) + __uint_as_float(both[1]), inv = den == 0.f ? 0.f : 1.f / den;       // a row that sees nothing: zeros
+    if (w0 + n32 < pairs) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const kv4_f32x4 x = no_number >> b & 1 ? kv4_f32x4{kv4_nan(), kv4_nan(), kv4_nan(), kv4_nan()} : kv4_f32x4{o[b][4 * q], o[b][4 * q + 1], o[b][4 * q + 2], o[b][4 * q + 3]} * inv;
+                kv4_store4<T, HD>(a, s, h, w0 + n32, 32 * b + 8 * q + 4 * hh, x);
+            }
     }
 }
 

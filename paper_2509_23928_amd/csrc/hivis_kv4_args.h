@@ -26,7 +26,7 @@ struct RowsArgs {
 
 struct Kv4AttnArgs {
     Kv4Dims d; int group, n_seqs, n_rows, max_rows, max_blocks, tiles; // group: query heads per key head; tiles: row tiles per sequence in the grid
-    float scale2;                                            // |softmax scale| times log2 e; negative ones negate the queries
+    float scale2;                                            // |softmax scale| times log2 e, not below the smallest normal number (infinity times zero has no value); negative ones negate the queries
     bool negate;
     const uint8_t* pool; const int *table, *row_start, *kv_len;
     const void* q; long long ldq; const unsigned long long* mask; void* out; long long ldo;

@@ -5,6 +5,7 @@
 #include "hivis_ops.h"
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -122,18 +123,17 @@ int kv4_read_launch(hipStream_t st, int type, const RowsArgs& a) {
     return HIVIS_OK;
 }
 
-// How a call is cut: kernel, pairs per workgroup in sixty-fours (rows kernel), row tiles of a sequence at most, workgroups.
-// The kernel is the one with the shorter estimate, in us; all from calls of 1 to 256 key heads, 1 to 2000 rows, 500 to 6000 cached rows:
+// How a call is cut: kernel, pairs per workgroup in sixty-fours (0: the stream kernel; 1: rows; 2: rows32), row tiles of a sequence at most, workgroups.
+// The kernel is the one with the shortest estimate, in us; all from calls of 1 to 256 key heads, 1 to 3000 rows, 64 to 6000 cached rows:
 //   stream: 8 us to open, merge and close (5.5 where no item is cut), and its 128-key units (16 pairs; two for each item) at the rate that a full chip reached;
 //   rows:   5.5 us, and the longer of its 64-key tiles one after the other (few workgroups: their latency) and all steps of 64 pairs x 64 keys at the full rate.
-// 61 rows of 28 heads over 3000 rows: stream 26 us, rows 112; 128 rows of 32 heads over 628: 17 and 21; 256 rows of 32 heads over themselves: 14 and 11;
-// 1024 rows of 32 heads: 57 and 32.  Two tiles of pairs per wavefront only in bf16 and only where the chip is full: 2000 rows x 4 of 32 heads 264 -> 182 us, but
-// 640 rows of 32 heads 21 -> 23 (fp32 spills: 377 -> 335 and 64 rows over 3000 rows 119 -> 176).
-struct Kv4Plan { bool rows; int rt, tiles, wgs; long long items; };
+// 61 rows of 28 heads over 3000 rows: stream 26 us, rows 112; 128 rows of 32 heads over 628: 16 and 21; 256 rows of 32 heads over themselves: 14, 11 and 12 (rows32);
+// 1024 rows of 32 heads: 57, 31 and 34; 2000 rows x 4 of 32 heads: rows 253, rows32 183 (fp32 383 and 344; heads of 64 dims 120 and 100).
+struct Kv4Plan { int rt, tiles, wgs; long long items; };
 static Kv4Plan kv4_plan_attend(const Kv4Dims& d, bool f32, int group, int n_seqs, int max_rows, int max_len) {
     const long long pairs = (long long)max_rows * group, sh = (long long)n_seqs * d.heads;
     const int form = (d.hd == 128 ? 0 : 1) + (f32 ? 2 : 0);
-    static const double unit_rate[4] = {350, 600, 260, 400}, tile_us[2][4] = {{1.45, 1.0, 2.3, 1.55}, {1.65, 1.35, 0, 0}}, step_rate[2][4] = {{248, 525, 173, 319}, {350, 605, 0, 0}};
+    static const double unit_rate[4] = {350, 600, 260, 400}, tile_us[2][4] = {{1.5, 0.9, 2.5, 1.45}, {1.7, 1.15, 3.3, 2.05}}, step_rate[2][4] = {{255, 560, 172, 335}, {365, 670, 192, 345}};
     const double keys = std::max(1.0, max_len - 0.5 * max_rows);         // that a row sees on average
     Kv4Plan p{};
     p.tiles = (int)((pairs + 15) / 16);
@@ -141,32 +141,32 @@ static Kv4Plan kv4_plan_attend(const Kv4Dims& d, bool f32, int group, int n_seqs
     p.wgs = (int)std::min<double>(256 * (f32 ? d.hd == 128 ? kv4_stream_per_cu<float, 128>() : kv4_stream_per_cu<float, 64>() : d.hd == 128 ? kv4_stream_per_cu<__bf16, 128>() : kv4_stream_per_cu<__bf16, 64>()),
                                   (double)p.items * (std::max(1, (int)(((long long)max_len + KV4_UNIT - 1) / KV4_UNIT)) + KV4_ITEM_COST));
     double best = (max_len > KV4_UNIT ? 8.0 : 5.5) + p.items * (keys / KV4_UNIT + 0.5 + KV4_ITEM_COST) / unit_rate[form];
-    for (int rt = 1; rt <= (f32 ? 1 : 2); ++rt) {
+    for (int rt = 1; rt <= 2; ++rt) {
         const long long tiles = (pairs + 64 * rt - 1) / (64 * rt);
         const double us = 5.5 + std::max((max_len + 63) / 64 * tile_us[rt - 1][form], sh * tiles * rt * (keys / 64 + 0.5) / step_rate[rt - 1][form]);
-        if (us < best) { best = us; p.rows = true; p.rt = rt; p.tiles = (int)tiles; }
+        if (us < best) { best = us; p.rt = rt; p.tiles = (int)tiles; }
     }
     return p;
 }
 // A workspace: counters, of the same number in every call (what one call leaves there is zero for the next, of whatever size), then partials
 constexpr int WS_COUNTERS = 1024 * sizeof(int);
-static long long kv4_space(const Kv4Plan& p, int hd) { return p.rows ? 16 : WS_COUNTERS + 2LL * p.wgs * 16 * (hd + 2) * 4; }
+static long long kv4_space(const Kv4Plan& p, int hd) { return p.rt ? 16 : WS_COUNTERS + 2LL * p.wgs * 16 * (hd + 2) * 4; }
 
 int kv4_attend_launch(hipStream_t st, int dtype, Kv4AttnArgs a, int max_rows, int max_len, void* ws) {
     const bool f32 = dtype == HIVIS_F32;
     const Kv4Plan p = kv4_plan_attend(a.d, f32, a.group, a.n_seqs, max_rows, max_len);
     const long long sh = ((long long)a.n_seqs * a.d.heads + 7) / 8 * 8;
     a.tiles = p.tiles; a.max_rows = max_rows; a.cnt = (int*)ws; a.ws = (float*)((char*)ws + WS_COUNTERS);
-#define KV4_ROWS_(T_, HD_, RT_)                                                                                                                               \
-    do {                                                                                                                                                      \
-        constexpr int lds_ = 2 * 64 * (kv4_vstride<HD_>() + kv4_kstride<HD_>()) + 3 * (3 + HD_ / 32) * 8;                                                     \
-        OP_TRY(hipFuncSetAttribute((const void*)kv4_rows_kernel<T_, HD_, RT_>, hipFuncAttributeMaxDynamicSharedMemorySize, lds_));                            \
-        hipLaunchKernelGGL((kv4_rows_kernel<T_, HD_, RT_>), dim3((unsigned)sh, p.tiles), dim3(256), lds_, st, a);                                             \
+#define KV4_ROWS_(KERNEL_, VSTRIDE_, HD_)                                                                                                      \
+    do {                                                                                                                                       \
+        constexpr int lds_ = 2 * 64 * (VSTRIDE_ + kv4_kstride<HD_>()) + 3 * (4 + HD_ / 32) * 8;                                                \
+        OP_TRY(hipFuncSetAttribute((const void*)KERNEL_, hipFuncAttributeMaxDynamicSharedMemorySize, lds_));                                   \
+        hipLaunchKernelGGL(KERNEL_, dim3((unsigned)sh, p.tiles), dim3(256), lds_, st, a);                                                      \
     } while (0)
 #define KV4_FORMS(T_, HD_)                                                                                      \
-    if (!p.rows) hipLaunchKernelGGL((kv4_stream_kernel<T_, HD_>), dim3(p.wgs), dim3(256), 0, st, a);            \
-    else if (p.rt == 1) KV4_ROWS_(T_, HD_, 1);                                                                  \
-    else if constexpr (sizeof(T_) == 2) KV4_ROWS_(T_, HD_, 2);
+    if (p.rt == 0) hipLaunchKernelGGL((kv4_stream_kernel<T_, HD_>), dim3(p.wgs), dim3(256), 0, st, a);            \
+    else if (p.rt == 1) KV4_ROWS_((kv4_rows_kernel<T_, HD_>), kv4_vstride<HD_>(), HD_);                         \
+    else KV4_ROWS_((kv4_rows32_kernel<T_, HD_>), kv4_vstride32<HD_>(), HD_);
     if (f32) { if (a.d.hd == 128) { KV4_FORMS(float, 128) } else { KV4_FORMS(float, 64) } }
     else { if (a.d.hd == 128) { KV4_FORMS(__bf16, 128) } else { KV4_FORMS(__bf16, 64) } }
 #undef KV4_FORMS
@@ -301,7 +301,7 @@ int hivis_kv4_attend(void* hip_stream, const hivis_kv4_attention* a) {
     CHECK(a->workspace_bytes >= need, "workspace of %lld bytes, %lld needed", (long long)a->workspace_bytes, need);
     if (int rc = check_devices({{a->pool, "pool"}, {a->table, "table"}, {a->row_start, "row_start"}, {a->kv_len, "kv_len"}, {a->q, "q"}, {a->mask, "mask"}, {a->out, "out"},
                                 {a->workspace, "workspace"}})) return rc;
-    k.group = a->n_q_heads / k.d.heads; k.n_seqs = a->n_seqs; k.n_rows = a->n_rows; k.max_blocks = a->max_blocks; k.scale2 = (float)(std::fabs(a->scale) * 1.4426950408889634); k.negate = a->scale < 0;
+    k.group = a->n_q_heads / k.d.heads; k.n_seqs = a->n_seqs; k.n_rows = a->n_rows; k.max_blocks = a->max_blocks; k.scale2 = std::max((float)(std::fabs(a->scale) * 1.4426950408889634), FLT_MIN); k.negate = a->scale < 0;
     k.pool = (const uint8_t*)a->pool; k.table = a->table; k.row_start = a->row_start; k.kv_len = a->kv_len; k.q = a->q; k.ldq = a->q_stride;
     k.mask = (const unsigned long long*)a->mask; k.out = a->out; k.ldo = a->out_stride;
     return kv4_attend_launch((hipStream_t)hip_stream, a->dtype, k, a->max_rows, a->max_len, a->workspace);
