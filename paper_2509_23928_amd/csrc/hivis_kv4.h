@@ -397,20 +397,17 @@ struct Kv4Sight {
     }
 };
 
-// Queries of RT tiles of pairs from pair p0 on (lanes behind the last repeat it), eight values of each in the order of dims that `dim` gives for lane quarter g and
+// Queries of 16 pairs from pair p0 on (lanes behind the last repeat it), eight values of each in the order of dims that `dim` gives for lane quarter g and
 // step j: as they lie in memory, and as operand parts
 template <typename T> struct Kv4Raw { kv4_u32x4 x[sizeof(T) / 2]; };
-template <typename T, int HD, int RT, typename Dim>
-__device__ inline void kv4_queries(const Kv4AttnArgs& a, const Kv4Seq& s, int h, int p0, int n16, int g, Dim dim, Kv4Raw<T> (&raw)[RT][HD / 32], Kv4Sight (&see)[RT]) {
+template <typename T, int HD, typename Dim>
+__device__ inline void kv4_queries(const Kv4AttnArgs& a, const Kv4Seq& s, int h, int p0, int n16, int g, Dim dim, Kv4Raw<T> (&raw)[HD / 32], Kv4Sight& see) {
+    const int pair = min(p0 + n16, s.pairs - 1), row = a.group == 1 ? pair : pair / a.group, hq = h * a.group + pair - row * a.group;
+    see.below = s.len - s.rows + (a.mask ? 0 : row + 1);
+    see.bits = a.mask ? a.mask[s.o0 + row] : 0;
+    const T* q = (const T*)a.q + (long long)(s.q0 + row) * a.ldq + (long long)hq * HD;
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        const int pair = min(p0 + 16 * t + n16, s.pairs - 1), row = a.group == 1 ? pair : pair / a.group, hq = h * a.group + pair - row * a.group;
-        see[t].below = s.len - s.rows + (a.mask ? 0 : row + 1);
-        see[t].bits = a.mask ? a.mask[s.o0 + row] : 0;
-        const T* q = (const T*)a.q + (long long)(s.q0 + row) * a.ldq + (long long)hq * HD;
-#pragma unroll
-        for (int j = 0; j < HD / 32; ++j) raw[t][j] = *(const Kv4Raw<T>*)(q + dim(g, j));
-    }
+    for (int j = 0; j < HD / 32; ++j) raw[j] = *(const Kv4Raw<T>*)(q + dim(g, j));
 }
 template <typename T, int NP>
 __device__ inline void kv4_query_part(bool negate, const Kv4Raw<T>& raw, kv4_bf16x8 (&f)[NP]) {
@@ -424,13 +421,6 @@ __device__ inline void kv4_query_part(bool negate, const Kv4Raw<T>& raw, kv4_bf1
         for (int e = 0; e < 8; ++e) { x[e] = __uint_as_float(raw.x[e >> 2][e & 3]); if (negate) x[e] = -x[e]; }
         kv4_parts<NP>(x, f);
     }
-}
-template <typename T, int HD, int RT, int NP>
-__device__ inline void kv4_query_parts(const Kv4AttnArgs& a, const Kv4Raw<T> (&raw)[RT][HD / 32], kv4_bf16x8 (&qf)[RT][HD / 32][NP]) {
-#pragma unroll
-    for (int t = 0; t < RT; ++t)
-#pragma unroll
-        for (int j = 0; j < HD / 32; ++j) kv4_query_part<T, NP>(a.negate, raw[t][j], qf[t][j]);
 }
 
 // One tile of pairs against NH halves of 16 keys, scores x (bit 16 c + 4 g + r of a lane's word: x[c][r]).
@@ -450,19 +440,32 @@ __device__ inline float kv4_top(const kv4_f32x4 (&x)[NH]) {
     for (int i = 1; i < 4 * NH; ++i) mx = fmaxf(mx, x[i >> 2][i & 3]);
     return mx;
 }
+// A weight's exponent is s - ref in one rounding, with s the exact product of a score and the scale, but ref a rounded one: beyond 2^24 the two are so far apart that
+// the weight of the largest score itself may be infinite or nothing.  There (`far`, of any lane) s is rounded first, as ref was.
+__device__ inline bool kv4_far(float ref) { return __any(fabsf(ref) > 0x1p24f && ref != KV4_REF0); }
+__device__ inline float kv4_rounded(float x, float scale2, float ref) {
+#pragma clang fp contract(off)
+    const float s = x * scale2;
+    return s - ref;
+}
 // ref follows a largest score of mx; what was added up so far follows it
 template <int NB>
-__device__ inline void kv4_follow(float mx, kv4_f32x4 (&o)[NB], float& ref, float& l) {
+__device__ inline void kv4_follow(float mx, kv4_f32x4 (&o)[NB], float& ref, float& l, bool& far) {
     const float to = fmaxf(ref, kv4_xmax(mx)), f = __builtin_amdgcn_exp2f(ref - to);
-    ref = to;
+    ref = to; far = kv4_far(to);
     l *= f;
 #pragma unroll
     for (int t = 0; t < NB; ++t) o[t] *= f;
 }
 // scores to weights in operand parts, and their sum
 template <int NH, int NP>
-__device__ inline void kv4_weights(const kv4_f32x4 (&x)[NH], float scale2, float ref, float& l, kv4_bf16x8 (&pf)[NH / 2][NP]) {
+__device__ inline void kv4_weights(kv4_f32x4 (&x)[NH], float scale2, float ref, bool far, float& l, kv4_bf16x8 (&pf)[NH / 2][NP]) {
     float p[4 * NH], s[4];
+    if (far) {
+#pragma unroll
+        for (int i = 0; i < 4 * NH; ++i) x[i >> 2][i & 3] = kv4_rounded(x[i >> 2][i & 3], scale2, ref);
+        scale2 = 1.f; ref = 0.f;
+    }
 #pragma unroll
     for (int i = 0; i < 4 * NH; ++i) p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i >> 2][i & 3], scale2, -ref));
 #pragma unroll
@@ -504,10 +507,11 @@ struct Kv4Partials {
 };
 
 // ---- few rows: bound by the cache's bytes, or by latency ----
-// An item is 16 pairs of one key head of one sequence, a unit KV4_UNIT keys of an item; the units of all items in a row are dealt to the workgroups in equal runs, so
-// lengths as different as they come leave no workgroup idle (one workgroup per item and split of a fixed length: 54 us for 48 conversations of 30 to 16000 rows, and 41 with
-// the best length, where most of a grid sized for the longest had nothing to do).  An item that lies in several runs is merged by the workgroup that
-// finishes last.
+// An item is 16 pairs of one key head of one sequence (32 pairs: 61 rows of 28 heads over 3075 rows 26 -> 49 us, and slower in 31 of 32 other shapes), a unit KV4_UNIT
+// keys of an item; the units of all items in a row are dealt to the workgroups in equal runs, so lengths as different as they come leave no workgroup idle
+// (one workgroup per item and split of a fixed length: 54 us for 48 conversations of 30 to 16000 rows, and 41 with the best length, where most of a grid sized for
+// the longest had nothing to do).  An item that lies in several runs is merged by the workgroup that finishes last.
+// (Eight wavefronts per workgroup and units of 256 keys: one token over 650 rows 8.1 -> 9.5 us, the 48 conversations 33.7 -> 40.6.)
 // The four wavefronts take tiles of 32 keys in turn, each with its own ref and sum.  A lane reads a quarter of a key's codes with one wide load and one scale byte,
 // and the next tile's while it multiplies this one; quarters are contiguous, so step j of the products takes dims g HD/4 + 8j of quarter g, and the keys
 // go from registers to the matrix cores.  Values go through the wavefront's own LDS tile (no barrier).
@@ -522,12 +526,12 @@ __device__ inline int kv4_div(int a, int b) {
     return r < 0 ? q - 1 : r >= b ? q + 1 : q;
 }
 struct Kv4Units {
-    const Kv4AttnArgs& a; int rt, lane, from, before, mine, upto, here;          // sequences from .. from + 63: units before them, of this lane's, up to and with it, of all 64
+    const Kv4AttnArgs& a; int lane, from, before, mine, upto, here;          // sequences from .. from + 63: units before them, of this lane's, up to and with it, of all 64
     Kv4Seq seq;                                              // this lane's
-    __device__ Kv4Units(const Kv4AttnArgs& a_, int rt_, int lane_) : a(a_), rt(rt_), lane(lane_), from(0), before(0) { load(); }
+    __device__ Kv4Units(const Kv4AttnArgs& a_, int lane_) : a(a_), lane(lane_), from(0), before(0) { load(); }
     __device__ void load() {
         seq = kv4_seq(a, min(from + lane, a.n_seqs - 1));
-        mine = from + lane < a.n_seqs ? (seq.pairs + 16 * rt - 1) / (16 * rt) * a.d.heads * (blocks(seq.len) + KV4_ITEM_COST) : 0;
+        mine = from + lane < a.n_seqs ? (seq.pairs + 15) / 16 * a.d.heads * (blocks(seq.len) + KV4_ITEM_COST) : 0;
         int x = mine;                                        // sums over the lanes below, within rows of 16, then across them
         x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false); x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
         x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false); x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
@@ -556,14 +560,13 @@ struct Kv4Units {
 template <typename T, int HD> constexpr int kv4_stream_per_cu() { return HD == 128 ? sizeof(T) == 4 ? 2 : 3 : sizeof(T) == 4 ? 3 : 4; }
 template <typename T, int HD>
 __global__ __launch_bounds__(256, (kv4_stream_per_cu<T, HD>())) void kv4_stream_kernel(Kv4AttnArgs a) {
-    constexpr int RT = 1;                                    // pairs of an item, in sixteens (32: 61 rows of 28 heads over 3075 rows 26 -> 49 us, and slower in 31 of 32 other shapes)
     constexpr int NP = sizeof(T) == 4 ? 3 : 1, STEPS = HD / 32, NB = HD / 16, VSTRIDE = kv4_vstride<HD>(), NW = 4;
     constexpr int MSTRIDE = HD + 4;                          // a pair's results in LDS: HD sums, ref, denominator
-    constexpr int VB = NW * 32 * VSTRIDE, MB = NW * 16 * MSTRIDE * 4, PLACE = 16 * RT * (HD + 2);
+    constexpr int VB = NW * 32 * VSTRIDE, MB = NW * 16 * MSTRIDE * 4, PLACE = 16 * (HD + 2);
     __shared__ __align__(16) char lds[VB > MB ? VB : MB];
     __shared__ int last;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    Kv4Units units(a, RT, threadIdx.x & 63);
+    Kv4Units units(a, threadIdx.x & 63);
     const int total = units.total(), per = kv4_div(total + (int)gridDim.x - 1, gridDim.x);
     const int bytes = kv4_chunk(HD, a.d.block);
     char* const vt = lds + wave * 32 * VSTRIDE;
@@ -578,8 +581,8 @@ __global__ __launch_bounds__(256, (kv4_stream_per_cu<T, HD>())) void kv4_stream_
     // ---- an item's part in this run: what it is, and the first requests to memory
     struct Item { Kv4Seq s; int seq, ti, h, nb, first, units, begins; } it;
     struct Tile { unsigned k[2][STEPS], v[2][STEPS], kb[2], vb[2]; int e[2]; } now;
-    Kv4Raw<T> raw[RT][STEPS];
-    Kv4Sight see[RT];
+    Kv4Raw<T> raw[STEPS];
+    Kv4Sight see;
     int k0, end, all, e0, e1, at;
     const int* row;
     auto entries = [&](int from, int lane) {                 // this wavefront's blocks, 64 tiles ahead: entry i of lane i
@@ -619,9 +622,9 @@ __global__ __launch_bounds__(256, (kv4_stream_per_cu<T, HD>())) void kv4_stream_
         it.first = max(0, from - KV4_ITEM_COST); it.units = max(0, from + n - KV4_ITEM_COST) - it.first;
         it.begins = pos - from + KV4_ITEM_COST;
         pos += n;
-        const int p0 = it.ti * 16 * RT;
+        const int p0 = it.ti * 16;
         // keys of the item: no pair of it sees one from `limit` on, all see those below `all`
-        const int limit = a.mask ? it.s.len : it.s.len - it.s.rows + min(p0 + 16 * RT - 1, it.s.pairs - 1) / a.group + 1;
+        const int limit = a.mask ? it.s.len : it.s.len - it.s.rows + min(p0 + 15, it.s.pairs - 1) / a.group + 1;
         all = it.s.len - it.s.rows + (a.mask ? 0 : p0 / a.group + 1);
         end = (int)min((long long)limit, (long long)(it.first + it.units) * KV4_UNIT);
         row = a.table + (size_t)(a.row_start ? it.seq : a.seq0 + it.seq) * a.max_blocks;
@@ -629,7 +632,7 @@ __global__ __launch_bounds__(256, (kv4_stream_per_cu<T, HD>())) void kv4_stream_
         at = 0;
         if (it.units == 0) { end = k0; return; }
         entries(k0, lane);
-        kv4_queries<T, HD, RT>(a, it.s, it.h, p0, n16, g, [](int g_, int j) { return g_ * (HD / 4) + 8 * j; }, raw, see);
+        kv4_queries<T, HD>(a, it.s, it.h, p0, n16, g, [](int g_, int j) { return g_ * (HD / 4) + 8 * j; }, raw, see);
         if (k0 < end) fetch(now, k0, 0, n16 * (HD / 2) + g * (HD / 8), n16 * (HD / 32) + g * (HD / 4) / 32);
     };
     open(threadIdx.x & 63);
@@ -638,18 +641,16 @@ __global__ __launch_bounds__(256, (kv4_stream_per_cu<T, HD>())) void kv4_stream_
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));                            // (what follows from it is not kept across items: 80 registers)
     const int lane = tid & 63, n16 = lane & 15, g = lane >> 4;
-    kv4_f32x4 o[RT][NB];
-    float ref[RT], l[RT];
-    unsigned no_number[RT];
+    kv4_f32x4 o[NB];
+    float ref = KV4_REF0, l = 0.f;
+    bool far = false;
+    unsigned no_number = 0;
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        ref[t] = KV4_REF0; l[t] = 0.f; no_number[t] = 0;
-#pragma unroll
-        for (int b = 0; b < NB; ++b) o[t][b] = kv4_f32x4{0.f, 0.f, 0.f, 0.f};
-    }
+    for (int b = 0; b < NB; ++b) o[b] = kv4_f32x4{0.f, 0.f, 0.f, 0.f};
     if (it.units) {
-    kv4_bf16x8 qf[RT][STEPS][NP];
-    kv4_query_parts<T, HD, RT, NP>(a, raw, qf);
+    kv4_bf16x8 qf[STEPS][NP];
+#pragma unroll
+    for (int j = 0; j < STEPS; ++j) kv4_query_part<T, NP>(a.negate, raw[j], qf[j]);
     for (; k0 < end; k0 += 32 * NW) {                        // (below 2^31: end is, and a step is short of the next block's last row)
         Tile t = now;
         if (++at == 64) { entries(k0 + 32 * NW, lane); at = 0; }
@@ -671,45 +672,38 @@ __global__ __launch_bounds__(256, (kv4_stream_per_cu<T, HD>())) void kv4_stream_
                     for (int i = 0; i < 64; ++i) {           // lane i: key i % 16, quarter i / 16
                         const unsigned dims = nk >> i & 1 ? 15u : nv >> i & 1 ? 1u << ((i >> 4) * (HD / 4) / 32) : 0u;
                         if (dims)
-#pragma unroll
-                            for (int r = 0; r < RT; ++r) if (see[r].of(k0 + 16 * half + (i & 15)) & 1) no_number[r] |= dims;
+                            if (see.of(k0 + 16 * half + (i & 15)) & 1) no_number |= dims;
                     }
                 if (!in || t.kb[half] == 255) t.kb[half] = 127;
                 if (!in || t.vb[half] == 255) t.vb[half] = 127;
             }
         }
-        kv4_f32x4 x[RT][2];
+        kv4_f32x4 x[2];
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             const float ks = __uint_as_float(t.kb[half] << 23), vs = __uint_as_float(t.vb[half] << 23);
 #pragma unroll
             for (int j = 0; j < STEPS; ++j) *(kv4_bf16x8*)(vt + (16 * half + n16) * VSTRIDE + (g * (HD / 4) + 8 * j) * 2) = kv4_expand(t.v[half][j], vs);
-#pragma unroll
-            for (int r = 0; r < RT; ++r) x[r][half] = kv4_f32x4{0.f, 0.f, 0.f, 0.f};
+            x[half] = kv4_f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int j = 0; j < STEPS; ++j) {
                 const kv4_bf16x8 kf = kv4_expand(t.k[half][j], ks);
 #pragma unroll
                 for (int p = NP - 1; p >= 0; --p)
-#pragma unroll
-                    for (int r = 0; r < RT; ++r) x[r][half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[r][j][p], x[r][half], 0, 0, 0);
+                    x[half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[j][p], x[half], 0, 0, 0);
             }
         }
-        kv4_bf16x8 pf[RT][1][NP];
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            if (!plain) kv4_hide(x[r], see[r].of(k0) & held, g);
-            const float mx = kv4_top(x[r]) * a.scale2;
-            if (__any(mx > ref[r] + KV4_SLACK)) kv4_follow(mx, o[r], ref[r], l[r]);
-            kv4_weights<2, NP>(x[r], a.scale2, ref[r], l[r], pf[r]);
-        }
+        kv4_bf16x8 pf[1][NP];
+        if (!plain) kv4_hide(x, see.of(k0) & held, g);
+        const float mx = kv4_top(x) * a.scale2;
+        if (__any(mx > ref + KV4_SLACK)) kv4_follow(mx, o, ref, l, far);
+        kv4_weights<2, NP>(x, a.scale2, ref, far, l, pf);
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
             const kv4_bf16x8 vf = kv4_vfrag<HD>(vt, b, lane);
 #pragma unroll
             for (int p = NP - 1; p >= 0; --p)
-#pragma unroll
-                for (int r = 0; r < RT; ++r) o[r][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[r][0][p], o[r][b], 0, 0, 0);
+                o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[0][p], o[b], 0, 0, 0);
         }
     }
     }
@@ -719,38 +713,35 @@ __global__ __launch_bounds__(256, (kv4_stream_per_cu<T, HD>())) void kv4_stream_
     if (done.units == 0) continue;
     // ---- the wavefronts' results, 16 pairs at a time
     asm volatile("" : "+v"(tid));
-    const int n16_ = tid & 15, g_ = tid >> 4 & 3, p0 = done.ti * 16 * RT, count = min(16 * RT, done.s.pairs - p0);
+    const int n16_ = tid & 15, g_ = tid >> 4 & 3, p0 = done.ti * 16, count = min(16, done.s.pairs - p0);
     const bool whole = done.units == done.nb, begins_here = done.first == 0;
     const unsigned part = place(blockIdx.x, begins_here);
+    l = kv4_xsum(l);
+    kv4_poison<NB>(no_number, o);
+    kv4_lds_barrier();
+    float* dst = mrg + (wave * 16 + n16_) * MSTRIDE;
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        l[r] = kv4_xsum(l[r]);
-        kv4_poison<NB>(no_number[r], o[r]);
-        kv4_lds_barrier();
-        float* dst = mrg + (wave * 16 + n16_) * MSTRIDE;
+    for (int b = 0; b < NB; ++b) *(kv4_f32x4*)(dst + 16 * b + 4 * g_) = o[b];
+    if (g_ == 0) *(float2*)(dst + HD) = make_float2(ref, l);
+    kv4_lds_barrier();
+    for (int i = tid; i < 16 * HD / 4; i += 256) {
+        const int pr = i / (HD / 4), c = 4 * (i % (HD / 4));
+        if (pr >= count) break;
+        float mx = KV4_REF0, den = 0.f;
+        kv4_f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int b = 0; b < NB; ++b) *(kv4_f32x4*)(dst + 16 * b + 4 * g_) = o[r][b];
-        if (g_ == 0) *(float2*)(dst + HD) = make_float2(ref[r], l[r]);
-        kv4_lds_barrier();
-        for (int i = tid; i < 16 * HD / 4; i += 256) {
-            const int pr = i / (HD / 4), c = 4 * (i % (HD / 4));
-            if (16 * r + pr >= count) break;
-            float mx = KV4_REF0, den = 0.f;
-            kv4_f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+        for (int w = 0; w < NW; ++w) mx = fmaxf(mx, mrg[(w * 16 + pr) * MSTRIDE + HD]);
 #pragma unroll
-            for (int w = 0; w < NW; ++w) mx = fmaxf(mx, mrg[(w * 16 + pr) * MSTRIDE + HD]);
-#pragma unroll
-            for (int w = 0; w < NW; ++w) {
-                const float* src = mrg + (w * 16 + pr) * MSTRIDE;
-                const float2 st = *(const float2*)(src + HD);
-                const float f = __builtin_amdgcn_exp2f(st.x - mx);
-                den += st.y * f; sum += *(const kv4_f32x4*)(src + c) * f;
-            }
-            if (whole) kv4_store4<T, HD>(a, done.s, done.h, p0 + 16 * r + pr, c, sum * (den == 0.f ? 0.f : 1.f / den));    // (a row that sees nothing: zeros)
-            else {
-                ws.put4(part + (16 * r + pr) * HD + c, sum);
-                if (c == 0) ws.put2(part + 16 * RT * HD + 2 * (16 * r + pr), mx, den);
-            }
+        for (int w = 0; w < NW; ++w) {
+            const float* src = mrg + (w * 16 + pr) * MSTRIDE;
+            const float2 st = *(const float2*)(src + HD);
+            const float f = __builtin_amdgcn_exp2f(st.x - mx);
+            den += st.y * f; sum += *(const kv4_f32x4*)(src + c) * f;
+        }
+        if (whole) kv4_store4<T, HD>(a, done.s, done.h, p0 + pr, c, sum * (den == 0.f ? 0.f : 1.f / den));    // (a row that sees nothing: zeros)
+        else {
+            ws.put4(part + pr * HD + c, sum);
+            if (c == 0) ws.put2(part + 16 * HD + 2 * pr, mx, den);
         }
     }
     kv4_lds_barrier();                                       // (the next item's values go where these results were)
@@ -765,7 +756,7 @@ __global__ __launch_bounds__(256, (kv4_stream_per_cu<T, HD>())) void kv4_stream_
     const int tid = threadIdx.x;
     const Item x = due_it[w];
     const Kv4Seq s = x.s;
-    const int h = x.h, p0 = x.ti * 16 * RT, count = min(16 * RT, s.pairs - p0);
+    const int h = x.h, p0 = x.ti * 16, count = min(16, s.pairs - p0);
     // (counted where the item begins: one at most begins in a run and goes on behind it)
     const int w0 = kv4_div(x.begins, per), parts = kv4_div(x.begins + x.nb - 1, per) - w0 + 1;
     if (tid == 0) last = __hip_atomic_fetch_add(&a.cnt[w0], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == parts - 1;
@@ -790,7 +781,7 @@ __global__ __launch_bounds__(256, (kv4_stream_per_cu<T, HD>())) void kv4_stream_
             for (int u = 0; u < 8; ++u) {
                 const int q = min(q0 + u * groups, parts - 1);
                 const unsigned from = place(w0 + q, q == 0);
-                v[u] = ws.get4(from + pr * HD + c); st[u] = ws.get2(from + 16 * RT * HD + 2 * pr);
+                v[u] = ws.get4(from + pr * HD + c); st[u] = ws.get2(from + 16 * HD + 2 * pr);
             }
             float to = mx;
 #pragma unroll
@@ -829,7 +820,7 @@ __global__ __launch_bounds__(256, (kv4_stream_per_cu<T, HD>())) void kv4_stream_
 // a tile ahead.
 template <typename T, int HD>
 __global__ __launch_bounds__(256, 2) void kv4_rows_kernel(Kv4AttnArgs a) {
-    constexpr int RT = 1, NP = sizeof(T) == 4 ? 3 : 1, STEPS = HD / 32, NB = HD / 16, KT = 64, VSTRIDE = kv4_vstride<HD>(), KSTRIDE = kv4_kstride<HD>();
+    constexpr int NP = sizeof(T) == 4 ? 3 : 1, STEPS = HD / 32, NB = HD / 16, KT = 64, VSTRIDE = kv4_vstride<HD>(), KSTRIDE = kv4_kstride<HD>();
     constexpr int BUF = KT * (VSTRIDE + KSTRIDE), NG = HD / 32;
     extern __shared__ __align__(16) char kv4_lds[];
     // Bits of a tile's keys: [0] any of the others; [1] not held; [2] the key's scale says NaN; [3 ..] those of the values' groups.  Three tiles in turn: written
@@ -842,10 +833,10 @@ __global__ __launch_bounds__(256, 2) void kv4_rows_kernel(Kv4AttnArgs a) {
     if (sh >= a.n_seqs * a.d.heads) return;
     const int h = sh % a.d.heads, seq = (int)((sh / a.d.heads + blockIdx.y) % a.n_seqs);
     const Kv4Seq s = kv4_seq(a, seq);
-    const int pairs = s.pairs, ti = (pairs + 64 * RT - 1) / (64 * RT) - 1 - (int)blockIdx.y, p0 = ti * 64 * RT, w0 = p0 + wave * 16 * RT;
+    const int pairs = s.pairs, ti = (pairs + 63) / 64 - 1 - (int)blockIdx.y, p0 = ti * 64, w0 = p0 + wave * 16;
     if (ti < 0) return;
-    const int limit = a.mask ? s.len : s.len - s.rows + min(p0 + 64 * RT - 1, pairs - 1) / a.group + 1;
-    const int mine = w0 >= pairs ? 0 : a.mask ? s.len : s.len - s.rows + min(w0 + 16 * RT - 1, pairs - 1) / a.group + 1;       // of this wavefront
+    const int limit = a.mask ? s.len : s.len - s.rows + min(p0 + 63, pairs - 1) / a.group + 1;
+    const int mine = w0 >= pairs ? 0 : a.mask ? s.len : s.len - s.rows + min(w0 + 15, pairs - 1) / a.group + 1;       // of this wavefront
     const int all = s.len - s.rows + (a.mask ? 0 : w0 / a.group + 1);
     const int* row = a.table + (size_t)(a.row_start ? seq : a.seq0 + seq) * a.max_blocks;
     const int bytes = kv4_chunk(HD, a.d.block);
@@ -874,22 +865,20 @@ __global__ __launch_bounds__(256, 2) void kv4_rows_kernel(Kv4AttnArgs a) {
         kb = sp[0]; vb = sp[a.d.block * (HD / 32)];
     };
     fetch(0);
-    kv4_bf16x8 qf[RT][STEPS][NP];
-    Kv4Sight see[RT];
+    kv4_bf16x8 qf[STEPS][NP];
+    Kv4Sight see;
     {
-        Kv4Raw<T> raw[RT][STEPS];
-        kv4_queries<T, HD, RT>(a, s, h, min(w0, pairs - 1), n16, g, [](int g_, int j) { return 32 * j + 8 * g_; }, raw, see);
-        kv4_query_parts<T, HD, RT, NP>(a, raw, qf);
+        Kv4Raw<T> raw[STEPS];
+        kv4_queries<T, HD>(a, s, h, min(w0, pairs - 1), n16, g, [](int g_, int j) { return 32 * j + 8 * g_; }, raw, see);
+    #pragma unroll
+    for (int j = 0; j < STEPS; ++j) kv4_query_part<T, NP>(a.negate, raw[j], qf[j]);
     }
-    kv4_f32x4 o[RT][NB];
-    float ref[RT], l[RT];
-    unsigned no_number[RT];
+    kv4_f32x4 o[NB];
+    float ref = KV4_REF0, l = 0.f;
+    bool far = false;
+    unsigned no_number = 0;
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        ref[t] = KV4_REF0; l[t] = 0.f; no_number[t] = 0;
-#pragma unroll
-        for (int b = 0; b < NB; ++b) o[t][b] = kv4_f32x4{0.f, 0.f, 0.f, 0.f};
-    }
+    for (int b = 0; b < NB; ++b) o[b] = kv4_f32x4{0.f, 0.f, 0.f, 0.f};
     int buf = 0, turn = 0;
     for (int k0 = 0; k0 < limit; k0 += KT, buf ^= 1, turn = turn == 2 ? 0 : turn + 1) {
         char* const kt = kv4_lds + buf * BUF; char* const vt = kt + KT * KSTRIDE;
@@ -909,18 +898,16 @@ __global__ __launch_bounds__(256, 2) void kv4_rows_kernel(Kv4AttnArgs a) {
         if (k0 + KT < limit) fetch(k0 + KT);
         if (threadIdx.x < 3 + NG) odd[turn == 0 ? 2 : turn - 1][threadIdx.x] = 0;
         if (k0 >= mine) continue;
-        kv4_f32x4 x[RT][4];
+        kv4_f32x4 x[4];
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-#pragma unroll
-            for (int r = 0; r < RT; ++r) x[r][c] = kv4_f32x4{0.f, 0.f, 0.f, 0.f};
+            x[c] = kv4_f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int j = 0; j < STEPS; ++j) {
                 const kv4_bf16x8 kf = *(const kv4_bf16x8*)(kt + (16 * c + n16) * KSTRIDE + (32 * j + 8 * g) * 2);
 #pragma unroll
                 for (int p = NP - 1; p >= 0; --p)
-#pragma unroll
-                    for (int r = 0; r < RT; ++r) x[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[r][j][p], x[r][c], 0, 0, 0);
+                    x[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[j][p], x[c], 0, 0, 0);
             }
         }
         const bool any = odd[turn][0] != 0, plain = k0 + KT <= all && !any;
@@ -929,18 +916,14 @@ __global__ __launch_bounds__(256, 2) void kv4_rows_kernel(Kv4AttnArgs a) {
             gone = odd[turn][1];
             for (int b = 0; b <= NG; ++b)
                 for (unsigned long long w = odd[turn][2 + b]; w; w &= w - 1) {
-#pragma unroll
-                    for (int r = 0; r < RT; ++r) if (see[r].of(k0 + __builtin_ctzll(w)) & 1) no_number[r] |= b ? 1u << (b - 1) : 15u;
+                    if (see.of(k0 + __builtin_ctzll(w)) & 1) no_number |= b ? 1u << (b - 1) : 15u;
                 }
         }
-        kv4_bf16x8 pf[RT][2][NP];
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            if (!plain) kv4_hide(x[r], see[r].of(k0) & ~gone, g);
-            const float mx = kv4_top(x[r]) * a.scale2;
-            if (__any(mx > ref[r] + KV4_SLACK)) kv4_follow(mx, o[r], ref[r], l[r]);
-            kv4_weights<4, NP>(x[r], a.scale2, ref[r], l[r], pf[r]);
-        }
+        kv4_bf16x8 pf[2][NP];
+        if (!plain) kv4_hide(x, see.of(k0) & ~gone, g);
+        const float mx = kv4_top(x) * a.scale2;
+        if (__any(mx > ref + KV4_SLACK)) kv4_follow(mx, o, ref, l, far);
+        kv4_weights<4, NP>(x, a.scale2, ref, far, l, pf);
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -948,20 +931,16 @@ __global__ __launch_bounds__(256, 2) void kv4_rows_kernel(Kv4AttnArgs a) {
                 const kv4_bf16x8 vf = kv4_vfrag<HD>(vt + 32 * k * VSTRIDE, b, lane);
 #pragma unroll
                 for (int p = NP - 1; p >= 0; --p)
-#pragma unroll
-                    for (int r = 0; r < RT; ++r) o[r][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[r][k][p], o[r][b], 0, 0, 0);
+                    o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[k][p], o[b], 0, 0, 0);
             }
     }
+    const float den = kv4_xsum(l), inv = den == 0.f ? 0.f : 1.f / den;    // a row that sees nothing: zeros
+    kv4_poison<NB>(no_number, o);
+    const int pr = w0 + n16;
+    if (pr < pairs) {
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        const float den = kv4_xsum(l[r]), inv = den == 0.f ? 0.f : 1.f / den;    // a row that sees nothing: zeros
-        kv4_poison<NB>(no_number[r], o[r]);
-        const int pr = w0 + 16 * r + n16;
-        if (pr < pairs) {
-#pragma unroll
-            for (int b = 0; b < NB; ++b)
-                kv4_store4<T, HD>(a, s, h, pr, 16 * b + 4 * g, o[r][b] * inv);
-        }
+        for (int b = 0; b < NB; ++b)
+            kv4_store4<T, HD>(a, s, h, pr, 16 * b + 4 * g, o[b] * inv);
     }
 }
 
@@ -1037,6 +1016,7 @@ __global__ __launch_bounds__(256, 2) void kv4_rows32_kernel(Kv4AttnArgs a) {
     }
     kv4_f32x16 o[NB];
     float ref = KV4_REF0, l = 0.f;
+    bool far = false;
     unsigned no_number = 0;
 #pragma unroll
     for (int b = 0; b < NB; ++b)
@@ -1102,20 +1082,25 @@ __global__ __launch_bounds__(256, 2) void kv4_rows32_kernel(Kv4AttnArgs a) {
             if (__any(mx > ref + KV4_SLACK)) {
                 const auto other = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
                 const float up = fmaxf(ref, fmaxf(__uint_as_float(other[0]), __uint_as_float(other[1]))), f = __builtin_amdgcn_exp2f(ref - up);
-                ref = up;
+                ref = up; far = kv4_far(up);
                 l *= f;
 #pragma unroll
                 for (int b = 0; b < NB; ++b)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) o[b][i] *= f;
             }
-            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+            float sum[4] = {0.f, 0.f, 0.f, 0.f}, scale2 = a.scale2, from = ref;
+            if (far) {
+#pragma unroll
+                for (int i = 0; i < KS / 2; ++i) x[i / 16][i & 15] = kv4_rounded(x[i / 16][i & 15], scale2, ref);
+                scale2 = 1.f; from = 0.f;
+            }
             kv4_bf16x8 pf[KS / 16][NP];
 #pragma unroll
             for (int k = 0; k < KS / 16; ++k) {
                 float e[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) { e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[k / 2][8 * (k & 1) + i], a.scale2, -ref)); sum[i & 3] += e[i]; }
+                for (int i = 0; i < 8; ++i) { e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[k / 2][8 * (k & 1) + i], scale2, -from)); sum[i & 3] += e[i]; }
                 kv4_parts<NP>(e, pf[k]);
             }
             l += (sum[0] + sum[1]) + (sum[2] + sum[3]);

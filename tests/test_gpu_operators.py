@@ -47,7 +47,8 @@ def special_rows(rng, shape):
 
 
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
-@pytest.mark.parametrize("heads,hd,block,rows,stride", [(1, 64, 16, 1, "plain"), (3, 128, 64, 33, "padded"), (4, 64, 32, 130, "heads first"), (8, 128, 256, 77, "plain"), (40, 128, 16, 9, "padded")])
+@pytest.mark.parametrize("heads,hd,block,rows,stride", [(1, 64, 16, 1, "plain"), (3, 128, 64, 33, "padded"), (4, 64, 32, 130, "heads first"), (8, 128, 256, 77, "plain"), (40, 128, 16, 9, "padded"), (2, 64, 32, 9001, "plain"),
+                                                         (3, 128, 64, 4099, "padded")])
 def test_append_and_read(dtype, heads, hd, block, rows, stride):
     rng = np.random.default_rng(rows * hd)
     dt = getattr(torch, dtype)
@@ -204,10 +205,10 @@ def masked(bits, length):
     return (new < 0) | ((np.asarray(bits, dtype=np.uint64)[:, None] >> np.maximum(new, 0).astype(np.uint64)) & np.uint64(1)).astype(bool)
 
 
-def attend(cache, rows, q, out=None, mask=None, scale=None, max_len=None, row_start=None, workspace=None, table=None):
+def attend(cache, rows, q, out=None, mask=None, scale=None, max_len=None, row_start=None, workspace=None, table=None, max_rows=None):
     out = torch.full_like(q, 9.0) if out is None else out
     starts = np.concatenate([[0], np.cumsum(rows)]) if row_start is None else row_start
-    top = max(list(rows) + [1])
+    top = max(list(rows) + [1]) if max_rows is None else max_rows
     length = max(cache.lens + [1]) if max_len is None else max_len
     if workspace is None:
         workspace = torch.zeros(hv.kv4_attend_bytes(cache.shape, q.shape[1], len(rows), top, length, q.dtype), dtype=torch.uint8, device=DEV)
@@ -254,6 +255,73 @@ def test_attend(kind, heads, group, hd, block, lens, rows):
     g = torch.Generator(device=DEV).manual_seed(len(lens))
     q = torch.randn(sum(rows), heads * group, hd, generator=g, device=DEV).to(getattr(torch, kind))
     check(cache, rows, q, attend(cache, rows, q), kind)
+
+
+@pytest.mark.parametrize("kind", ["float32", "bfloat16"])
+@pytest.mark.parametrize("pairs,length", [(16, 1 << 20), (2000, 64), (1000000, 1), (1000000, 300)])
+@pytest.mark.parametrize("heads,group,hd,block,lens,rows", SHAPES)
+def test_attend_forms(kind, heads, group, hd, block, lens, rows, pairs, length):
+    """The same calls as launched for other sizes: which kernel runs is a matter of the promised rows and lengths, the results are not."""
+    cache = Cache(lens, heads, hd, block, seed=sum(lens))
+    g = torch.Generator(device=DEV).manual_seed(len(lens))
+    q = torch.randn(sum(rows), heads * group, hd, generator=g, device=DEV).to(getattr(torch, kind))
+    check(cache, rows, q, attend(cache, rows, q, max_rows=max(max(rows), pairs // group), max_len=length), kind)
+
+
+@pytest.mark.parametrize("kind", ["float32", "bfloat16"])
+@pytest.mark.parametrize("heads,group,hd", [(2, 1, 64), (1, 3, 128)])
+def test_attend_many_sequences(kind, heads, group, hd):
+    """More sequences than lanes, empty ones among them; trees of 64 rows in enough sequences for the prompts' kernels."""
+    rng = random.Random(hd)
+    lens = [rng.choice((0, 1, 16, 40, rng.randrange(200))) for _ in range(150)]
+    rows = [min(n, rng.choice((0, 1, 1, 3))) for n in lens]
+    cache = Cache(lens, heads, hd, 16, seed=8)
+    q = torch.randn(sum(rows), heads * group, hd, device=DEV).to(getattr(torch, kind))
+    check(cache, rows, q, attend(cache, rows, q), kind)
+    cache = Cache([64 + s % 9 for s in range(96)], 8, 64, 32, seed=9)
+    bits = [tree_bits(64, s) for s in range(96)]
+    q = torch.randn(96 * 64, 16, 64, device=DEV).to(getattr(torch, kind))
+    check(cache, [64] * 96, q, attend(cache, [64] * 96, q, mask=sum(bits, [])), kind, see=[masked(b, n) for b, n in zip(bits, cache.lens)])
+
+
+@pytest.mark.parametrize("kind", ["float32", "bfloat16"])
+def test_attend_scores_of_any_size(kind):
+    """Scores far below zero alone, and a scale of zero and below it."""
+    cache = Cache([40], 1, 64, 16, seed=12)
+    q = torch.randn(3, 1, 64, device=DEV).to(getattr(torch, kind))
+    for scale in (0.0, -0.125):
+        for pairs in (3, 1000000):
+            check(cache, [3], q, attend(cache, [3], q, scale=scale, max_rows=pairs), kind, scale=scale)
+    cache.parts[0][:] = (cache.parts[0] & 0x77) | 0x11                         # keys above zero: the scores of queries below it are far below it, all of them
+    cache.upload()
+    q = -q.abs() * 2.0 ** 70
+    out = attend(cache, [3], q, scale=2.0 ** 40)
+    assert torch.isfinite(out).all() and (out != 0).any()
+    check(cache, [3], q, out, kind, scale=2.0 ** 40)
+
+
+def test_workspace_is_left_as_found():
+    """One workspace for calls of any sizes, of attention and of log probabilities, in any order: as with one of their own."""
+    calls = []
+    for lens, rows, heads, group in (([700], [1], 4, 1), ([3000, 90], [3, 8], 8, 2), ([130] * 5, [1] * 5, 2, 4), ([50], [50], 1, 1)):
+        cache = Cache(lens, heads, 128, 32, seed=len(lens))
+        q = torch.randn(sum(rows), heads * group, 128, device=DEV)
+        calls.append(lambda ws, c=cache, r=rows, q=q: [attend(c, r, q, workspace=ws)])
+    for rows, vocab in ((1, 90000), (40, 20000), (3, 30000)):
+        x, tokens = torch.randn(rows, vocab, device=DEV), i32(np.arange(rows)[:, None])
+
+        def call(ws, x=x, tokens=tokens, rows=rows, vocab=vocab):
+            lp, ids, tlp = torch.empty(rows, 1, device=DEV), torch.empty(rows, 4, dtype=torch.int32, device=DEV), torch.empty(rows, 4, device=DEV)
+            hv.logprobs(x, tokens, lp, None, ids, tlp, workspace=torch.zeros(hv.logprobs_bytes(rows, vocab, 4), dtype=torch.uint8, device=DEV) if ws is None else ws, stream=stream())
+            return [lp, ids, tlp]
+        calls.append(call)
+    want = [c(None) for c in calls]
+    ws = torch.zeros(1 << 25, dtype=torch.uint8, device=DEV)
+    order = [i for i in range(len(calls))] * 6
+    random.Random(3).shuffle(order)
+    for i in order:
+        for a, b in zip(want[i], calls[i](ws)):
+            assert torch.equal(a, b), i
 
 
 @pytest.mark.parametrize("kind", ["float32", "bfloat16"])
@@ -422,7 +490,7 @@ def check_logprobs(x, tokens, temperature, top, got):
 
 
 @pytest.mark.parametrize("kind", ["float32", "bfloat16"])
-@pytest.mark.parametrize("rows,vocab,n,top,temperature", [(1, 1, 1, 1, 1.0), (3, 5, 2, 5, 0.5), (2, 1024, 1, 20, 1.0), (6, 32000, 1, 5, 1.0), (1, 152064, 3, 32, 0.7), (130, 4097, 1, 0, 2.0), (17, 50257, 4, 7, 1.3), (300, 999, 2, 32, 1.0)])
+@pytest.mark.parametrize("rows,vocab,n,top,temperature", [(1, 1, 1, 1, 1.0), (3, 5, 2, 5, 0.5), (2, 1024, 1, 20, 1.0), (6, 32000, 1, 5, 1.0), (1, 152064, 3, 32, 0.7), (130, 4097, 1, 0, 2.0), (17, 50257, 4, 7, 1.3), (300, 999, 2, 32, 1.0), (2, 3001, 300, 3, 1.0)])
 def test_logprobs(kind, rows, vocab, n, top, temperature):
     g = torch.Generator(device=DEV).manual_seed(vocab)
     x = (3 * torch.randn(rows, vocab, generator=g, device=DEV)).to(getattr(torch, kind))
