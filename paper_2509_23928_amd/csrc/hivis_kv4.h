@@ -307,7 +307,7 @@ __global__ __launch_bounds__(256) void kv4_move_kernel(Kv4Dims d, uint8_t* mem, 
 }
 
 // ---- attention ------------------------------------------------------------------------------------------------------------------------------
-// Both kernels multiply alike.  A tile of 16 (row, query head) pairs of one key head, row by row, is the N dimension of
+// The kernels multiply alike.  A tile of 16 (row, query head) pairs of one key head, row by row, is the N dimension of
 //   S^T[key][pair] = K Q^T          mfma 16x16x32, 16 keys as rows
 //   O^T[dim][pair] += V^T P^T       a lane's weights of keys 4g .. 4g+3 of two 16-key halves are its operand as they come out of S^T (contractions take any
 //                                   order that both operands share); V^T comes from row-major bf16 in LDS through the transposing read.
@@ -382,7 +382,7 @@ __device__ inline Kv4Seq kv4_seq(const Kv4AttnArgs& a, int s) {
     Kv4Seq x;
     if (a.row_start) { x.q0 = x.o0 = a.row_start[s]; x.rows = a.row_start[s + 1] - x.q0; x.len = a.kv_len[s]; }
     else { x.q0 = s * a.qrows; x.o0 = s * a.m; x.rows = a.m; x.len = a.kv_len[a.seq0 + s] + a.len_add; }
-    x.len = min(x.len, a.max_blocks << a.d.shift);
+    x.len = max(0, min(x.len, a.max_blocks << a.d.shift));
     if (x.o0 < 0 || x.rows < 0 || x.rows > a.n_rows - x.o0) x.rows = 0;      // (no rows of this call)
     x.pairs = min(x.rows, a.max_rows) * a.group;
     return x;

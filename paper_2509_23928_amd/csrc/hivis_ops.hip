@@ -64,13 +64,12 @@ int check_shape(const hivis_kv4_shape* s, Kv4Dims* d) {
 
 int check_rows(const void* k, const void* v, int dtype, const Kv4Dims& d, long long row, long long head, int n) {
     CHECK(dtype == HIVIS_F32 || dtype == HIVIS_BF16, "dtype %d unknown", dtype);
-    CHECK(n >= 0 && (long long)n * d.heads <= 0x7fffffffLL, "n_rows %d x n_kv_heads %d", n, d.heads);
+    CHECK(n >= 0 && n <= 1 << 30 && (long long)n * d.heads <= 0x7fffffffLL, "n_rows %d (2^30 at most) x n_kv_heads %d", n, d.heads);
     CHECK(row % 8 == 0 && head % 8 == 0, "row and head strides must be multiples of 8 values (%lld, %lld)", row, head);
     CHECK(row >= 0 && head >= d.hd, "strides %lld, %lld: rows of a head are head_dim values side by side", row, head);
     CHECK(aligned(k, 16) && aligned(v, 16), "rows must start at multiples of 16 bytes");
     return HIVIS_OK;
 }
-
 
 }  // namespace
 

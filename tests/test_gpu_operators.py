@@ -400,6 +400,18 @@ def test_attend_blocks_outside_the_pool():
     check(cache, [2], q, out, "float32", see=[on])
 
 
+@pytest.mark.parametrize("pairs", [2, 2000, 1000000])
+def test_attend_lengths_that_are_none(pairs):
+    """Cached rows below zero, and more than the table holds: as zero, and as many as it holds."""
+    cache = Cache([64, 0, 0], 1, 64, 16, seed=4)
+    q = torch.randn(6, 1, 64, device=DEV)
+    cache.lens = [2 ** 31 - 1, -2 ** 31, -1]
+    out = attend(cache, [2, 2, 2], q, max_len=64, max_rows=pairs)
+    assert not out[2:].any()
+    cache.lens = [64, 0, 0]
+    check(cache, [2, 2, 2], q, out, "float32")
+
+
 def test_attend_rows_outside_the_call():
     """A row_start that does not fit the rows of q: the sequence is left out."""
     cache = Cache([40, 40], 1, 64, 16, seed=4)

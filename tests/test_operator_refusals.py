@@ -56,6 +56,7 @@ def test_rows(call):
         return LIB.hivis_kv4_read(None, C.byref(s), dtype, pool, n, slots, k, v, row, head)
     refused(run(dtype=2), "dtype")
     refused(run(n=-1), "n_rows")
+    refused(run(n=(1 << 30) + 1), "n_rows")
     refused(run(row=132), "strides")
     refused(run(head=66), "strides")
     refused(run(head=56), "strides")
