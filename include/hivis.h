@@ -294,7 +294,7 @@ int hivis_kv4_plan(void *hip_stream, int32_t n_seqs, int32_t max_blocks, int32_t
 
 /* Rows into the cache.  k, v: HIVIS_F32 or HIVIS_BF16, head h of row r at r * row_stride + h * head_stride (in values, both
  * multiples of 8; the same for k and v), starting at multiples of 16 bytes.  n_rows <= 2^30; slots [n_rows]: a slot outside the pool (-1)
- * leaves its row out.  Two rows with the same slot leave one of the two in each group of 32 dims.
+ * leaves its row out.  Two rows of a call with the same slot leave a mixture of both there (nowhere else).
  * Errors: EINVAL, EHIP. */
 int hivis_kv4_append(void *hip_stream, const hivis_kv4_shape *shape, int32_t dtype, const void *k, const void *v, int64_t row_stride, int64_t head_stride, int32_t n_rows,
                      const int32_t *slots, void *pool);
