@@ -230,6 +230,7 @@ int hivis_kv4_plan(void* hip_stream, int32_t n_seqs, int32_t max_blocks, int32_t
     if (int rc = check_shape(&shape, &d)) return rc;
     CHECK(n_seqs >= 1, "n_seqs %d", n_seqs);
     CHECK(max_blocks >= 1 && (long long)max_blocks * block_tokens <= 0x7fffffffLL, "max_blocks %d: a sequence's positions must be in 0..2^31-1", max_blocks);
+    CHECK((long long)n_seqs * max_blocks <= 0x7fffffffLL, "n_seqs %d x max_blocks %d: a table has fewer than 2^31 entries", n_seqs, max_blocks);
     CHECK(max_rows >= 0, "max_rows %d", max_rows);
     CHECK(keep && add && held && table && free_list && row_start && status && (slots || max_rows == 0), "null argument");
     if (int rc = check_devices({{keep, "keep"}, {add, "add"}, {held, "held"}, {table, "table"}, {free_list, "free_list"}, {row_start, "row_start"}, {slots, "slots"},

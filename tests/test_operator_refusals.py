@@ -42,6 +42,7 @@ def test_plan():
     refused(call(T=20), "block_tokens")
     refused(call(pool=0), "n_blocks")
     refused(call(rows=-1), "max_rows")
+    refused(call(n=1 << 20, blocks=1 << 12), "n_seqs")
     for name in ("keep", "table", "slots", "status"):
         refused(call(**{name: None}), "null")
 
