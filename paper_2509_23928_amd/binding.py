@@ -34,6 +34,9 @@ class Kv4Shape(C.Structure):
     """hivis_kv4_shape: a pool of the paged cache in 4 bits, Kv4Shape(n_kv_heads, head_dim, block_tokens, n_blocks)."""
     _fields_ = [(n, C.c_int32) for n in ("n_kv_heads", "head_dim", "block_tokens", "n_blocks")]
 
+    def _bytes(self):                        # as hivis_kv4_pool_bytes, without its checks: the call that follows makes them
+        return self.n_blocks * self.n_kv_heads * self.block_tokens * (self.head_dim + self.head_dim // 16)
+
 
 class hivis_kv4_attention(C.Structure):
     _fields_ = [("cache", Kv4Shape), ("dtype", C.c_int32), ("n_q_heads", C.c_int32), ("n_seqs", C.c_int32), ("n_rows", C.c_int32), ("max_blocks", C.c_int32),
@@ -226,7 +229,7 @@ def _kv4_rows(shape, pool, slots, k, v):
     if rows and one != 1:
         _refuse("k, v: the values of a head are not side by side")
     # a dimension of one element has any stride
-    return (_dtype(k.dtype), _tensor(pool, "uint8", (kv4_pool_bytes(shape),), "pool"), _tensor(slots, "int32", (rows,), "slots"), rows, row if rows > 1 else 0,
+    return (_dtype(k.dtype), _tensor(pool, "uint8", (shape._bytes(),), "pool"), _tensor(slots, "int32", (rows,), "slots"), rows, row if rows > 1 else 0,
             head if heads > 1 and rows else hd)
 
 
@@ -260,7 +263,7 @@ def kv4_attend(shape, pool, table, row_start, kv_len, q, out, *, max_rows, max_l
     if rows and (ldq[2] != 1 or ldo[2] != 1 or (hq > 1 and (ldq[1] != hd or ldo[1] != hd))):
         _refuse("q, out: the heads of a row are not side by side")
     t = _tensor
-    a = hivis_kv4_attention(shape, _dtype(q.dtype), hq, n, rows, blocks, max_rows, max_len, hd ** -0.5 if scale is None else scale, t(pool, "uint8", (kv4_pool_bytes(shape),), "pool"),
+    a = hivis_kv4_attention(shape, _dtype(q.dtype), hq, n, rows, blocks, max_rows, max_len, hd ** -0.5 if scale is None else scale, t(pool, "uint8", (shape._bytes(),), "pool"),
                             t(table, "int32", (n, blocks), "table"), t(row_start, "int32", (n + 1,), "row_start"), t(kv_len, "int32", (n,), "kv_len"), q.data_ptr(),
                             ldq[0] if rows > 1 else hq * hd, t(mask, "int64", (rows,), "mask"), out.data_ptr(), ldo[0] if rows > 1 else hq * hd,
                             t(workspace, "uint8", None, "workspace"), workspace.shape[0])
