@@ -947,18 +947,17 @@ __global__ __launch_bounds__(256, 2) void kv4_rows_kernel(Kv4AttnArgs a) {
 // ---- more rows than fill the chip ----
 // As above with products of 32 x 32: 32 pairs per wavefront, 128 per workgroup, for half the reads of LDS per product.  Half as many instructions of the matrix cores leave
 // more room for vector work beside them (per SIMD, 128 multiply-adds beside the products of two wavefronts: 842 cycles with 16 x 16, 723 with 32 x 32).  Four
-// prompts of 641 to 3008 rows, 32 heads: 163 us, 0.81 PFLOP/s (tiles of 16 x 16, two per wavefront: 175; scores a tile ahead of the weights 173; two workgroups' work
+// prompts of 641 to 3008 rows, 32 heads: 160 us, 0.82 PFLOP/s (tiles of 16 x 16, two per wavefront: 175; scores a tile ahead of the weights 173; two workgroups' work
 // in one, keys shared: 223; 32 keys per tile and three wavefronts per SIMD: 177; 64 pairs per wavefront: registers spill).
 // A lane has one pair and, of every eight keys, the four of its half.  Keys of KS at a time go through the softmax (32 where the operand parts of 64 would not
-// fit the registers).
+// fit the registers).  What GROUP products read from LDS is requested a group ahead (left to the compiler, each read stood before its product: 168 -> 160 us).
 template <typename T, int HD>
 __global__ __launch_bounds__(256, 2) void kv4_rows32_kernel(Kv4AttnArgs a) {
     constexpr int NP = sizeof(T) == 4 ? 3 : 1, KS = sizeof(T) == 4 ? 32 : 64, STEPS = HD / 16, NB = HD / 32, KT = 64, VSTRIDE = kv4_vstride32<HD>(), KSTRIDE = kv4_kstride<HD>();
-    constexpr int BUF = KT * (VSTRIDE + KSTRIDE), NG = HD / 32, NC = HD / 32;
+    constexpr int BUF = KT * (VSTRIDE + KSTRIDE), NG = HD / 32, NC = HD / 32, GROUP = NP == 1 ? 4 : 2;
     extern __shared__ __align__(16) char kv4_lds[];
-    // Bits of a tile's keys: [0] any of the next two; [1] not held; [2] the key's scale says NaN; [3] any of the others; [4 ..] the scale of a value's group does.
-    // Three tiles in turn: written before a tile's barrier, read behind it, cleared behind the next one.
-    unsigned long long (*const odd)[4 + NG] = (unsigned long long (*)[4 + NG])(kv4_lds + 2 * BUF);
+    // Bits of a tile's keys as above
+    unsigned long long (*const odd)[3 + NG] = (unsigned long long (*)[3 + NG])(kv4_lds + 2 * BUF);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n32 = lane & 31, hh = lane >> 5;
     const int sh = blockIdx.x;
     if (sh >= a.n_seqs * a.d.heads) return;
@@ -971,7 +970,7 @@ __global__ __launch_bounds__(256, 2) void kv4_rows32_kernel(Kv4AttnArgs a) {
     const int all = s.len - s.rows + (a.mask ? 0 : w0 / a.group + 1);
     const int* row = a.table + (size_t)(a.row_start ? seq : a.seq0 + seq) * a.max_blocks;
     const int bytes = kv4_chunk(HD, a.d.block);
-    if (threadIdx.x < 3 * (4 + NG)) ((unsigned long long*)odd)[threadIdx.x] = 0;
+    if (threadIdx.x < 3 * (3 + NG)) ((unsigned long long*)odd)[threadIdx.x] = 0;
     __syncthreads();
 
     // a wavefront's 16 keys lie in one block: the address is the same for all lanes but for an offset
@@ -979,7 +978,7 @@ __global__ __launch_bounds__(256, 2) void kv4_rows32_kernel(Kv4AttnArgs a) {
     const unsigned at_code = (lane >> 2) * (HD / 2) + kq * (HD / 8), at_scale = (lane >> 2) * (HD / 32) + kq * (HD / 4) / 32;
     struct Part { unsigned c[NC], b; } kp, vp;               // a quarter of a key and of a value: codes, scale
     bool in;
-    auto entry = [&](int k0) { const int key = k0 + 16 * wave; return key < s.len ? kv4_scalar(row[key >> a.d.shift]) : -1; };
+    auto entry = [&](int k0) { const int key = k0 + 16 * wave; return key < s.len ? row[key >> a.d.shift] : -1; };
     int next = entry(0);                                     // block of the tile that is fetched next, a tile ahead of it
     auto get = [&](Part& t, const uint8_t* c, int r) {
         const uint8_t* p = c + r * (HD / 2) + at_code;
@@ -988,7 +987,7 @@ __global__ __launch_bounds__(256, 2) void kv4_rows32_kernel(Kv4AttnArgs a) {
         t.b = (c + a.d.block * HD + r * (HD / 32))[at_scale];
     };
     auto fetch = [&](int k0) {
-        const int e = next, r = (k0 + 16 * wave) & (a.d.block - 1);
+        const int e = kv4_scalar(next), r = (k0 + 16 * wave) & (a.d.block - 1);
         next = entry(k0 + KT);
         in = e >= 0 && e < a.d.n_blocks;
         const uint8_t* c = a.pool + ((size_t)(in ? e : 0) * a.d.heads + h) * bytes;
@@ -1033,8 +1032,9 @@ __global__ __launch_bounds__(256, 2) void kv4_rows32_kernel(Kv4AttnArgs a) {
             const bool held = in && k0 + kr < s.len;
             if (!held || kp.b == 255 || vp.b == 255) {
                 const unsigned long long bit = 1ull << kr;
-                if (!held || kp.b == 255) { atomicOr(&w[0], bit); atomicOr(&w[held ? 2 : 1], bit); }
-                if (held && vp.b == 255) { atomicOr(&w[3], bit); atomicOr(&w[4 + kq * (HD / 4) / 32], bit); }
+                atomicOr(&w[0], bit);
+                if (!held || kp.b == 255) atomicOr(&w[held ? 2 : 1], bit);
+                if (held && vp.b == 255) atomicOr(&w[3 + kq * (HD / 4) / 32], bit);
             }
             const float ks = __uint_as_float((held && kp.b != 255 ? kp.b : 127u) << 23), vs = __uint_as_float((held && vp.b != 255 ? vp.b : 127u) << 23);
 #pragma unroll
@@ -1045,28 +1045,54 @@ __global__ __launch_bounds__(256, 2) void kv4_rows32_kernel(Kv4AttnArgs a) {
         }
         __syncthreads();
         if (k0 + KT < limit) fetch(k0 + KT);
-        if (threadIdx.x < 4 + NG) odd[turn == 0 ? 2 : turn - 1][threadIdx.x] = 0;
+        if (threadIdx.x < 3 + NG) odd[turn == 0 ? 2 : turn - 1][threadIdx.x] = 0;
         if (k0 >= mine) continue;
-        const bool any = w[0] != 0;
-        unsigned long long gone = 0;
-        if (any) { gone = w[1]; noted(w[2], 15u, k0); }
-        if (w[3] != 0)
-            for (int b = 0; b < NG; ++b) noted(w[4 + b], 1u << b, k0);
-        const bool plain = k0 + KT <= all && !any;
-        const unsigned long long vis = plain ? 0 : (see.of(k0) & ~gone) >> 4 * hh;
+        const unsigned long long any = w[0];                 // (asked for before the keys, looked at behind their products)
+        unsigned long long vis = 0;
+        bool plain = k0 + KT <= all;
 #pragma unroll
         for (int part = 0; part < KT / KS; ++part) {
             kv4_f32x16 x[KS / 32];
+            kv4_bf16x8 f[2][GROUP], vf[2][GROUP];
 #pragma unroll
-            for (int c = 0; c < KS / 32; ++c) {
+            for (int c = 0; c < KS / 32; ++c)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) x[c][i] = 0.f;
+            auto keys = [&](int first, kv4_bf16x8 (&to)[GROUP]) {
 #pragma unroll
-                for (int j = 0; j < STEPS; ++j) {
-                    const kv4_bf16x8 kf = *(const kv4_bf16x8*)(kt + (part * KS + 32 * c + n32) * KSTRIDE + (16 * j + 8 * hh) * 2);
+                for (int i = first; i < first + GROUP; ++i)
+                    to[i - first] = *(const kv4_bf16x8*)(kt + (part * KS + 32 * (i % (KS / 32)) + n32) * KSTRIDE + (16 * (i / (KS / 32)) + 8 * hh) * 2);
+            };
+            auto values = [&](int first, kv4_bf16x8 (&to)[GROUP]) {
 #pragma unroll
-                    for (int p = NP - 1; p >= 0; --p) x[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[j][p], x[c], 0, 0, 0);
+                for (int i = first; i < first + GROUP; ++i) {
+                    typedef __attribute__((address_space(3))) kv4_s16x4* lds_p;
+                    const char* src = vt + from_v + (part * KS + 16 * (i / NB)) * VSTRIDE + 64 * (i % NB);
+                    union { kv4_s16x4 s[2]; kv4_bf16x8 f; } v;
+                    v.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_p)src);
+                    v.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_p)(src + 8 * VSTRIDE));
+                    to[i - first] = v.f;
                 }
+            };
+            keys(0, f[0]);
+#pragma unroll
+            for (int i = 0; i < KS / 32 * STEPS; i += GROUP) {
+                if (i + GROUP < KS / 32 * STEPS) keys(i + GROUP, f[i / GROUP + 1 & 1]); else values(0, vf[0]);
+#pragma unroll
+                for (int u = 0; u < GROUP; ++u)
+#pragma unroll
+                    for (int p = NP - 1; p >= 0; --p)
+                        x[(i + u) % (KS / 32)] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i / GROUP & 1][u], qf[(i + u) / (KS / 32)][p], x[(i + u) % (KS / 32)], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (part == 0 && (any || !plain)) {
+                unsigned long long gone = 0;
+                if (any) {
+                    gone = w[1]; noted(w[2], 15u, k0);
+                    for (int b = 0; b < NG; ++b) noted(w[3 + b], 1u << b, k0);
+                }
+                plain = false;
+                vis = (see.of(k0) & ~gone) >> 4 * hh;
             }
             if (!plain)
 #pragma unroll
@@ -1105,17 +1131,14 @@ __global__ __launch_bounds__(256, 2) void kv4_rows32_kernel(Kv4AttnArgs a) {
             }
             l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
 #pragma unroll
-            for (int k = 0; k < KS / 16; ++k)
+            for (int i = 0; i < KS / 16 * NB; i += GROUP) {
+                if (i + GROUP < KS / 16 * NB) values(i + GROUP, vf[i / GROUP + 1 & 1]);
 #pragma unroll
-                for (int b = 0; b < NB; ++b) {
-                    typedef __attribute__((address_space(3))) kv4_s16x4* lds_p;
-                    const char* src = vt + from_v + (part * KS + 16 * k) * VSTRIDE + 64 * b;
-                    union { kv4_s16x4 s[2]; kv4_bf16x8 f; } v;
-                    v.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_p)src);
-                    v.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_p)(src + 8 * VSTRIDE));
+                for (int u = 0; u < GROUP; ++u)
 #pragma unroll
-                    for (int p = NP - 1; p >= 0; --p) o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v.f, pf[k][p], o[b], 0, 0, 0);
-                }
+                    for (int p = NP - 1; p >= 0; --p)
+                        o[(i + u) % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i / GROUP & 1][u], pf[(i + u) / NB][p], o[(i + u) % NB], 0, 0, 0);
+            }
         }
     }
     const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);

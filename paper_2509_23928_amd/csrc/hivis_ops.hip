@@ -158,7 +158,7 @@ int kv4_attend_launch(hipStream_t st, int dtype, Kv4AttnArgs a, int max_rows, in
     a.tiles = p.tiles; a.max_rows = max_rows; a.cnt = (int*)ws; a.ws = (float*)((char*)ws + WS_COUNTERS);
 #define KV4_ROWS_(KERNEL_, VSTRIDE_, HD_)                                                                                                      \
     do {                                                                                                                                       \
-        constexpr int lds_ = 2 * 64 * (VSTRIDE_ + kv4_kstride<HD_>()) + 3 * (4 + HD_ / 32) * 8;                                                \
+        constexpr int lds_ = 2 * 64 * (VSTRIDE_ + kv4_kstride<HD_>()) + 3 * (3 + HD_ / 32) * 8;                                                \
         OP_TRY(hipFuncSetAttribute((const void*)KERNEL_, hipFuncAttributeMaxDynamicSharedMemorySize, lds_));                                   \
         hipLaunchKernelGGL(KERNEL_, dim3((unsigned)sh, p.tiles), dim3(256), lds_, st, a);                                                      \
     } while (0)
