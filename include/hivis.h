@@ -325,7 +325,7 @@ typedef struct {
     const void *q;           /* [rows][n_q_heads][head_dim], rows q_stride values apart */
     int64_t q_stride;
     const uint64_t *mask;    /* [rows], or NULL */
-    void *out;               /* as q, rows out_stride values apart; rows outside row_start's ranges are left as they were */
+    void *out;               /* as q (not in its memory), rows out_stride values apart; rows outside row_start's ranges are left as they were */
     int64_t out_stride;
     void *workspace;
     int64_t workspace_bytes;

@@ -98,6 +98,29 @@ def test_cycles(monkeypatch, name, block):
     print(name, block, sbs.summary())
 
 
+@pytest.mark.parametrize("switch", ["HIVIS_FUSED=0", "HIVIS_ATTN_ELECT=0", "HIVIS_WIDE_GEMM=0", "HIVIS_ATTN_SHARED_MIN=8"])
+@pytest.mark.parametrize("name", ["bf16 four sequences", "bf16 no visual rows, short prompt"])
+def test_cycles_under_switches(monkeypatch, name, switch):
+    monkeypatch.setenv(*switch.split("="))
+    cfg = CONFIGS[name]()
+    w = synth.make_weights(cfg, seed=4)
+    vis, ids = synth.make_prompt(cfg, seed=4)
+    hv = HeldHivis(cfg, w, kv4_block=32)
+    monkeypatch.setattr(parity_utils, "HivisOracle", following(HivisOracle, hv))
+    sbs = parity_utils.SideBySide(cfg, w, hv, vis, ids)
+    for _ in range(3):
+        sbs.cycle(cfg.K)
+    hv.close()
+
+
+def test_one_launch_per_pass_is_refused(monkeypatch):
+    monkeypatch.setenv("HIVIS_PERSISTENT", "1")
+    cfg = small_bf16()
+    with pytest.raises(HivisError) as e:
+        Hivis(cfg, synth.make_weights(cfg, seed=4), kv4_block=32)
+    assert e.value.code == HIVIS_EINVAL and "HIVIS_PERSISTENT" in str(e.value)
+
+
 def test_accepted_drafts_move_the_lengths(monkeypatch):
     """Drafts that the target accepts: sequences of a batch grow apart, and rows of rejected drafts give their places back."""
     cfg = small_bf16(batch=3, K=4, n_vis=20, n_text=11)
@@ -199,7 +222,8 @@ def test_pool_of_blocks():
         assert max(before[0]) + 5 > 48 and cycles >= 2
         after = hv.kv_lengths()
         assert all((a == b).all() for a, b in zip(before, after))
-        hv.set_drafts([[0]] * 2) if max(before[0]) + 2 <= 48 else None
+        if max(before[0]) + 2 <= 48:
+            hv.set_drafts([[0]] * 2)
     with pytest.raises(HivisError) as e:
         Hivis(cfg, w, kv4_block=16, kv4_blocks=2).prefill(vis, ids)
     assert e.value.code == HIVIS_ECAP
