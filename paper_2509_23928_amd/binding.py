@@ -192,7 +192,7 @@ def _tensor(t, kind, shape, name):
     """Address of a contiguous tensor of this type and shape (shape None: any one-dimensional; t None: no tensor)."""
     if t is None:
         return None
-    if _kind(t.dtype) != kind:
+    if _kinds.get(t.dtype) != kind and _kind(t.dtype) != kind:
         _refuse(f"{name}: {t.dtype} instead of {kind}")
     if t.shape != shape and (shape is not None or len(t.shape) != 1):
         _refuse(f"{name}: shape {tuple(t.shape)} instead of {shape}")
@@ -255,10 +255,11 @@ def kv4_attend_bytes(shape, n_q_heads, n_seqs, max_rows, max_len, dtype):
 def kv4_attend(shape, pool, table, row_start, kv_len, q, out, *, max_rows, max_len, workspace, scale=None, mask=None, stream=None):
     """hivis_kv4_attend: attention of q [rows][n_q_heads][head_dim] over the cached rows, to out (as q).  table [n_seqs][max_blocks], row_start
     [n_seqs + 1], kv_len [n_seqs] int32; mask [rows] int64 or None; scale None: 1 / sqrt(head_dim)."""
-    if len(q.shape) != 3 or q.shape[2] != shape.head_dim or out.shape != q.shape or out.dtype != q.dtype or len(table.shape) != 2:
-        _refuse(f"q {tuple(q.shape)} and out {tuple(out.shape)}: [rows][n_q_heads][{shape.head_dim}] of one type; table [n_seqs][max_blocks]")
-    rows, hq, hd = q.shape
-    n, blocks = table.shape
+    of_q, of_table = q.shape, table.shape
+    if len(of_q) != 3 or of_q[2] != shape.head_dim or out.shape != of_q or out.dtype != q.dtype or len(of_table) != 2:
+        _refuse(f"q {tuple(of_q)} and out {tuple(out.shape)}: [rows][n_q_heads][{shape.head_dim}] of one type; table [n_seqs][max_blocks]")
+    rows, hq, hd = of_q
+    n, blocks = of_table
     ldq, ldo = q.stride(), out.stride()
     if rows and (ldq[2] != 1 or ldo[2] != 1 or (hq > 1 and (ldq[1] != hd or ldo[1] != hd))):
         _refuse("q, out: the heads of a row are not side by side")
